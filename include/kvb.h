@@ -21,6 +21,15 @@
  *   kvb_sparse_attn_layer  the repair forward's attention of one layer over
  *                       the patched cache (Eq. 2), with its prebuilt plan
  *
+ * and decodes from it:
+ *
+ *   kvb_qk_norm_rope    norms and rotation of a step's queries and keys
+ *   kvb_cache8_append   rows of K and V into a cache held in 8 bits
+ *   kvb_cache8_read     ... and back as values
+ *   kvb_cache8_attn     attention of the last tokens over that cache, with the
+ *                       accumulated weight of each block
+ *   kvb_cache8_evict    the blocks of least accumulated weight leave
+ *
  * plus the host helpers that prepare their inputs (rotation tables, row
  * flags, the threshold-activated probe of Sec. 7.4) and the cache-population
  * kernels (RoPE at absolute positions, KIVI quantisation, chunk importance;
@@ -436,6 +445,202 @@ kvb_status kvb_sparse_attn_layer(int32_t layer, int32_t n_layers, int32_t n_q_he
                                  const void* plans, size_t plans_bytes, float softmax_scale,
                                  kvb_dtype out_dtype, void* out, void* workspace,
                                  size_t workspace_bytes, void* stream);
+
+/* ---- decoding from a prepared prompt -------------------------------------
+ * What follows the prompt's cache: a decode step takes the projection's
+ * queries and keys through kvb_qk_norm_rope, adds the new rows to an 8-bit
+ * cache (kvb_cache8_append) and attends over it (kvb_cache8_attn); now and
+ * then kvb_cache8_evict drops the blocks that had the least attention.  The
+ * prompt itself is packed by one kvb_cache8_append over the patched bf16 cache.
+ * These entry points joined version 7 without changing what was there. */
+
+/* Scaling of rotary positions for contexts longer than the ones a model was
+ * trained on (HOST struct).  With omega_i = theta^(-2i/rot_dim), s = factor and
+ * r_i = original_len * omega_i / (2 pi) (the rotations pair i makes within the
+ * original length), the pair's frequency is
+ *   NONE    omega_i
+ *   LINEAR  omega_i / s                                  (position interpolation)
+ *   NTK     (theta * s^(rot_dim / (rot_dim - 2)))^(-2i/rot_dim)
+ *   PARTS   g omega_i + (1 - g) omega_i / s,  g = clamp((r_i - low) / (high - low), 0, 1)
+ *   INDEX   (1 - h) omega_i + h omega_i / s,  h = clamp((i - i0) / max(i1 - i0, 0.001), 0, 1),
+ *           i0 = max(floor(x(high)), 0), i1 = min(ceil(x(low)), rot_dim - 1),
+ *           x(r) = (rot_dim / 2) ln(original_len / (2 pi r)) / ln(theta)
+ * (PARTS and INDEX interpolate the slow pairs and keep the fast ones: by
+ * rotations, or by the pair's index between the two rotation counts).  Cosine
+ * and sine are multiplied by attn_factor (1 = none). */
+typedef enum {
+  KVB_ROPE_NONE = 0, KVB_ROPE_LINEAR = 1, KVB_ROPE_NTK = 2, KVB_ROPE_PARTS = 3, KVB_ROPE_INDEX = 4
+} kvb_rope_kind;
+typedef struct {
+  int32_t kind;         /* kvb_rope_kind */
+  double factor;        /* s >= 1 */
+  double original_len;  /* PARTS and INDEX: tokens of the trained context, > 0 */
+  double low, high;     /* PARTS and INDEX: rotations, 0 < low < high */
+  double attn_factor;   /* > 0 */
+} kvb_rope_scaling;
+
+/* Rotation table of absolute positions with scaled frequencies (HOST only, no
+ * GPU): cos_out / sin_out f32 [n][rot_dim/2] for pos[n], evaluated in double
+ * (angles of far positions keep their accuracy) and rounded once.  With kind
+ * NONE and attn_factor 1 (or scaling NULL) it equals kvb_rope_delta_table.
+ * Errors: KVB_EINVAL (null pointer, n < 0, rot_dim not even and positive,
+ * theta <= 0 or, for INDEX, <= 1, NTK with rot_dim 2, a scaling outside the
+ * ranges above). */
+kvb_status kvb_rope_scaled_table(double theta, int32_t rot_dim, const kvb_rope_scaling* scaling,
+                                 const int32_t* pos, int32_t n, float* cos_out, float* sin_out);
+
+/* Channels that rotate together: HALF pairs i with i + rot_dim/2, INTERLEAVED
+ * pairs 2i with 2i + 1. */
+typedef enum { KVB_PAIR_HALF = 0, KVB_PAIR_INTERLEAVED = 1 } kvb_pairing;
+
+/* Norms of the queries and keys of each head and their rotation, in one pass.
+ * For token t, head h of q (n_q_heads) or k (n_kv_heads), x its head_dim values:
+ *   y_c = x_c * w_c / sqrt(sum_c x_c^2 / head_dim + eps)   (w NULL: y = x)
+ *   out_a = y_a c_i - y_b s_i,  out_b = y_b c_i + y_a s_i
+ * for the pairs (a, b) of the first rot_dim channels, with (c, s) row pos[t] of
+ * the tables (f32 [table_len][rot_dim/2]); the other channels are y.  Arithmetic
+ * is float, rounded once to dtype (KVB_BF16 or KVB_F32, of inputs and outputs
+ * alike).  A token whose position lies outside [0, table_len) is written as NaN.
+ * Element (t, h, c) of each tensor lies at t * token_stride + h * head_stride +
+ * c, strides in elements, multiples of 8: the input may be one projection's
+ * output with queries, keys and values side by side, k_out a layer of the cache.
+ * Outputs may be their inputs (the same address and strides).  rot_dim 0
+ * (tables and pos NULL) only norms; n_q_heads or n_kv_heads may be 0 (its
+ * pointers NULL).  q_weight, k_weight: f32 [head_dim].  pos: i32 [n_tokens].
+ * Errors: KVB_EINVAL, KVB_EUNSUPPORTED (head_dim not a multiple of 8 up to 256,
+ * rot_dim not a multiple of 8). */
+kvb_status kvb_qk_norm_rope(int64_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads,
+                            int32_t head_dim, kvb_dtype dtype, const void* q,
+                            int64_t q_token_stride, int64_t q_head_stride, const void* k,
+                            int64_t k_token_stride, int64_t k_head_stride, const float* q_weight,
+                            const float* k_weight, float eps, const int32_t* pos,
+                            const float* table_cos, const float* table_sin, int32_t table_len,
+                            int32_t rot_dim, kvb_pairing pairing, void* q_out,
+                            int64_t q_out_token_stride, int64_t q_out_head_stride, void* k_out,
+                            int64_t k_out_token_stride, int64_t k_out_head_stride, void* stream);
+
+/* A cache held in 8 bits (HOST struct).  One table row for each (sequence, kv
+ * head) names pool blocks of B tokens; a sequence of len tokens holds floor(len
+ * / B) full blocks, each with one float scale for K and one for V, and its last
+ * len mod B tokens as bfloat16 in the tails, so every value is rounded to 8 bits
+ * once, when its block is full:
+ *   KVB_I8    scale = amax / 127 (float), code = clamp(rint(x / scale), -127, 127),
+ *             rint of the exact quotient, ties to even
+ *   KVB_E4M3  scale = the smallest power of two with amax / scale <= 448, code =
+ *             the e4m3 number (1.4.3, no infinities) nearest to x / scale, ties to even
+ * with amax the largest magnitude of the block; amax 0: scale 0 and codes 0; a
+ * block with an infinity or NaN: scale NaN and codes 0 (it reads as NaN).
+ * Device arrays, with a leading [L] where a call takes n_layers (one pool for
+ * all layers; lens is shared):
+ *   table           i32  [L][n_seqs][Hkv][max_blocks]   entry j: the block of tokens jB .. jB+B-1
+ *   lens            i32  [n_seqs]
+ *   k_codes         u8   [n_blocks][B][d]
+ *   v_codes         u8   [n_blocks][d][B]               (channel-major)
+ *   k_scale/v_scale f32  [n_blocks]
+ *   k_tail          bf16 [L][n_seqs][Hkv][B][d]
+ *   v_tail          bf16 [L][n_seqs][Hkv][d][B]         (channel-major)
+ * An entry is needed once its block is full.  An entry outside [0, n_blocks)
+ * is no block: its tokens are neither written nor read, nor seen by the
+ * attention.  lens[b] is at most max_blocks * B + B - 1 (tokens past that are
+ * neither written, read nor seen) and a negative one counts as 0. */
+typedef enum { KVB_I8 = 0, KVB_E4M3 = 1 } kvb_code;
+typedef struct {
+  int32_t n_blocks;    /* blocks of the pool */
+  int32_t n_kv_heads;  /* Hkv */
+  int32_t head_dim;    /* d: 64 or 128 */
+  int32_t block_len;   /* B: 16, 32, 64 or 128 */
+  int32_t code;        /* kvb_code */
+  int32_t max_blocks;  /* entries of a table row */
+} kvb_cache8_layout;
+
+/* Add rows to the cache.  Sequence b gets rows cu_new[b] .. cu_new[b+1]-1 of k
+ * and v (bf16; element (layer, row, head, channel) at layer * layer_stride + row
+ * * token_stride + head * head_stride + channel, strides in elements, multiples
+ * of 8: a projection's output or the stitched cache [L][Hkv][T][d]).  lens[b] is
+ * the length AFTER the call (the caller counts the new tokens in, as
+ * kvb_cache8_attn wants them): the rows become tokens lens[b] - n_new ..
+ * lens[b]-1.  Blocks that become full are quantised from the tail and the new
+ * rows; the rows of the last block go to the tails, whose other rows keep what
+ * they hold.  A sequence without new rows is left alone, one with lens[b] < n_new
+ * as well.  max_new bounds the new rows of a sequence (it sizes the grid).
+ * cu_new i32 [n_seqs+1].  A table must not name a block twice.
+ * Errors: KVB_EINVAL, KVB_EUNSUPPORTED (layout). */
+kvb_status kvb_cache8_append(const kvb_cache8_layout* layout, int32_t n_layers, int32_t n_seqs,
+                             const int32_t* cu_new, int32_t max_new, const uint16_t* k,
+                             const uint16_t* v, int64_t layer_stride, int64_t token_stride,
+                             int64_t head_stride, const int32_t* table, const int32_t* lens,
+                             uint8_t* k_codes, float* k_scale, uint8_t* v_codes, float* v_scale,
+                             uint16_t* k_tail, uint16_t* v_tail, void* stream);
+
+/* Read the last rows of each sequence back as values (code * scale; tail rows as
+ * they are): tokens lens[b] - n .. lens[b]-1 with n = cu_out[b+1] - cu_out[b],
+ * into rows cu_out[b] .. of k_out and v_out (out_dtype KVB_F32, or KVB_BF16
+ * rounded to nearest even; strides as in kvb_cache8_append).  A sequence with
+ * lens[b] < n is left alone.  max_out bounds n.
+ * Errors: as kvb_cache8_append. */
+kvb_status kvb_cache8_read(const kvb_cache8_layout* layout, int32_t n_layers, int32_t n_seqs,
+                           const int32_t* cu_out, int32_t max_out, const int32_t* table,
+                           const int32_t* lens, const uint8_t* k_codes, const float* k_scale,
+                           const uint8_t* v_codes, const float* v_scale, const uint16_t* k_tail,
+                           const uint16_t* v_tail, kvb_dtype out_dtype, void* k_out, void* v_out,
+                           int64_t layer_stride, int64_t token_stride, int64_t head_stride,
+                           void* stream);
+
+/* Workspace bytes kvb_cache8_attn needs (pure function; 0 for invalid sizes). */
+size_t kvb_cache8_attn_workspace_bytes(const kvb_cache8_layout* layout, int32_t n_q_heads,
+                                       int32_t n_seqs, int32_t n_queries, int32_t max_queries,
+                                       int32_t max_len, int32_t with_weights);
+
+/* Attention of the last tokens of each sequence over one layer of the cache.
+ * Sequence b has queries cu_q[b] .. cu_q[b+1]-1, which are its last n_q tokens
+ * (already in the cache): with g = floor(h * Hkv / Hq), query i of them sees the
+ * tokens u <= lens[b] - n_q + i, and
+ *   lse[q][h] = ln sum_u exp(softmax_scale * q . K[g][u])
+ *   out[q][h] = sum_u exp(softmax_scale * q . K[g][u] - lse) V[g][u]
+ * over the cache's values.  A query that sees nothing gets out 0 and lse
+ * -infinity.  q, out: bf16 [n_queries][Hq][d]; lse: f32 [n_queries][Hq] (NULL for
+ * none); a query outside every sequence's range is not written.  weights_out (NULL
+ * for none): f32 [n_seqs][Hkv][max_blocks], the accumulated attention weight of
+ * each block: weights_in (NULL: zeros; may be the same array) plus, for block j,
+ * the sum over the sequence's queries, the query heads of the kv head and the
+ * block's tokens of exp(softmax_scale * q . k - lse); the tokens of the tails
+ * count for entry floor(lens[b] / B) where there is one.
+ * Scores are 16-bit products summed in float (codes are exact in fp16; a query
+ * is scaled to fp16 by a power of two), softmax, weights and sums in float; the
+ * probabilities enter the product with V as fp16, those of the tails as the sum of two bfloat16.
+ * max_queries bounds n_q, max_len bounds lens (they size the grid; results
+ * do not depend on max_len but for the order of the sums).  Deterministic.
+ * workspace: at least kvb_cache8_attn_workspace_bytes; calls that share it must be ordered.
+ * Errors: KVB_EINVAL (incl. workspace too small, Hq % Hkv != 0), KVB_EUNSUPPORTED
+ * (layout). */
+kvb_status kvb_cache8_attn(const kvb_cache8_layout* layout, int32_t n_q_heads, int32_t n_seqs,
+                           const int32_t* cu_q, int32_t n_queries, int32_t max_queries,
+                           int32_t max_len, const uint16_t* q, const int32_t* table,
+                           const int32_t* lens, const uint8_t* k_codes, const float* k_scale,
+                           const uint8_t* v_codes, const float* v_scale, const uint16_t* k_tail,
+                           const uint16_t* v_tail, float softmax_scale, uint16_t* out, float* lse,
+                           const float* weights_in, float* weights_out, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+/* Eviction by accumulated attention weight.  A table row (layer, sequence, kv
+ * head) with nb = floor(lens[b] / B) > budget full blocks keeps its first n_first
+ * and last n_recent blocks and, of the others, the budget - n_first - n_recent of
+ * largest weight (ties: the lower index; -0 equals +0; NaN ranks below every
+ * number); the order of what is kept stays.  table_out's row holds the kept
+ * entries, then the old entries from nb on (the tail's and later ones), then the
+ * dropped ones, so that the sequence can fill them again: a row stays a
+ * permutation of itself.  weights_out moves along, 0 for the dropped.  lens_out
+ * [b] = lens[b] - (nb - budget) * B.  A row with nb <= budget is copied.  Tails
+ * and pool are not touched: tokens keep the positions they were rotated at.
+ * weights, weights_out: f32 [L][n_seqs][Hkv][max_blocks].  No output may be an
+ * input.  Only the layout's n_kv_heads, block_len and max_blocks are used.
+ * Errors: KVB_EINVAL (incl. n_first + n_recent > budget, an output that is an
+ * input). */
+kvb_status kvb_cache8_evict(const kvb_cache8_layout* layout, int32_t n_layers, int32_t n_seqs,
+                            int32_t budget, int32_t n_first, int32_t n_recent,
+                            const int32_t* table, const int32_t* lens, const float* weights,
+                            int32_t* table_out, int32_t* lens_out, float* weights_out,
+                            void* stream);
 
 #ifdef __cplusplus
 }

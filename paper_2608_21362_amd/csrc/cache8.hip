@@ -1,0 +1,472 @@
+// The 8-bit cache: rows in (kvb_cache8_append), rows out (kvb_cache8_read) and the
+// eviction of blocks (kvb_cache8_evict).
+//
+// Append and read stream: bfloat16 in, one byte out (or the reverse), HBM-bound.
+// A workgroup takes one block of one (layer, sequence, kv head) and one of K and V.
+// It holds the block in registers between the maximum and the codes, so rows are
+// read once.  V goes through LDS, because its blocks are channel-major.
+#include "kvb_device.h"
+#include "kvb_internal.h"
+
+namespace kvb {
+namespace {
+
+typedef __attribute__((ext_vector_type(2))) _Float16 half2_t;
+
+// The tokens [first, first + n) of a sequence that a call adds or reads, and the
+// blocks they touch.
+struct Span {
+  int64_t before;  // tokens before the call's rows
+  int64_t end;     // tokens after the last of them
+  int64_t j0;      // first block touched
+  int32_t blocks;  // blocks touched, 0: nothing to do
+};
+__device__ __forceinline__ Span span_of(const int32_t* cu, const int32_t* lens, int b, int B) {
+  Span s;
+  const int64_t n = (int64_t)cu[b + 1] - cu[b];
+  s.end = lens[b];
+  s.before = s.end - n;
+  s.j0 = s.before / B;
+  s.blocks = n > 0 && s.before >= 0 ? (int32_t)((s.end - 1) / B - s.j0 + 1) : 0;
+  return s;
+}
+
+// ---- codes ----------------------------------------------------------------
+
+// The scale of a block from its largest magnitude (bf16 bits; 0x7F80 and above: an
+// infinity or NaN) and what a value is multiplied with on the way to its code.  The
+// quotients of a block whose scale may be subnormal are formed at 2^64 times the size.
+struct Scale {
+  float scale, lift, s, inv;  // stored; x * lift; scale * lift; about 1 / s
+  int shift;                  // e4m3: code value = x * 2^shift
+};
+template <int CODE>
+__device__ __forceinline__ Scale scale_of(uint32_t amax_bits) {
+  Scale r;
+  const float amax = __uint_as_float(amax_bits << 16);
+  r.lift = 1.f, r.s = 1.f, r.inv = 0.f, r.shift = 0;
+  if (amax_bits == 0) {
+    r.scale = 0.f;
+  } else if (amax_bits >= 0x7F80u) {
+    r.scale = __builtin_nanf("");
+  } else if constexpr (CODE == KVB_I8) {
+    r.scale = amax / 127.0f;
+    r.lift = amax < 0x1p-60f ? 0x1p64f : 1.f;
+    r.s = r.scale * r.lift;
+    r.inv = 1.f / r.s;
+  } else {
+    const float m = __builtin_amdgcn_frexp_mantf(amax);  // [0.5, 1)
+    const int e = __builtin_amdgcn_frexp_expf(amax) - (m <= 0.875f ? 9 : 8);
+    r.scale = __builtin_ldexpf(1.f, e);
+    r.shift = -e;
+  }
+  return r;
+}
+
+// int8: clamp(rint(x / scale)) of the exact quotient.  t is within 1e-5 of it, so rint
+// can only be wrong that near a half; there the remainder decides: x - c s is exact in
+// one fused operation (both are multiples of the smaller one's last bit, and the
+// difference is small).
+__device__ __forceinline__ int code_i8(float x, const Scale& r) {
+  const float xl = x * r.lift, t = xl * r.inv;
+  float c = rintf(t);
+  if (__builtin_expect(!(fabsf(t - c) < 0.499f), 0)) {
+    const float rest = __builtin_fmaf(-c, r.s, xl), half = 0.5f * r.s;
+    const float step = rest > 0.f ? 1.f : -1.f;
+    if (fabsf(rest) > half || (fabsf(rest) == half && ((int)c & 1))) c += step;
+  }
+  return (int)fminf(fmaxf(c, -127.f), 127.f);
+}
+
+// codes of 4 values as the bytes of a word
+template <int CODE>
+__device__ __forceinline__ uint32_t codes4(const float* x, const Scale& r) {
+  if constexpr (CODE == KVB_I8) {
+    return (uint32_t)(code_i8(x[0], r) & 255) | (uint32_t)(code_i8(x[1], r) & 255) << 8 |
+           (uint32_t)(code_i8(x[2], r) & 255) << 16 | (uint32_t)code_i8(x[3], r) << 24;
+  } else {
+    // exact product with a power of two, then one rounding to nearest even
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(__builtin_ldexpf(x[0], r.shift),
+                                            __builtin_ldexpf(x[1], r.shift), 0, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(__builtin_ldexpf(x[2], r.shift),
+                                        __builtin_ldexpf(x[3], r.shift), w, true);
+    return (uint32_t)w;
+  }
+}
+
+// the values of the 4 codes of a word, as code * scale
+template <int CODE>
+__device__ __forceinline__ void values4(uint32_t w, float scale, float* x) {
+  if constexpr (CODE == KVB_I8) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = (float)(int8_t)(w >> (8 * i)) * scale;
+  } else {
+    typedef __attribute__((ext_vector_type(2))) float f2;
+    const f2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false);
+    const f2 b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+    x[0] = a[0] * scale, x[1] = a[1] * scale, x[2] = b[0] * scale, x[3] = b[1] * scale;
+  }
+}
+
+// ---- append ---------------------------------------------------------------
+
+// The tail rows [from, to) of block j of one sequence and head, from the new rows.
+template <int D, int B>
+__device__ __forceinline__ void write_tail(int is_v, uint16_t* tail, const uint16_t* rows,
+                                           int64_t token_stride, int from, int to) {
+  constexpr int PPR = D / 8;  // 16-byte pieces of a row
+  for (int i = threadIdx.x; i < (to - from) * PPR; i += blockDim.x) {
+    const int u = i / PPR, c = i % PPR * 8;
+    const uint4 x = *reinterpret_cast<const uint4*>(rows + (int64_t)u * token_stride + c);
+    if (!is_v) {
+      *reinterpret_cast<uint4*>(tail + (from + u) * D + c) = x;
+    } else {
+      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) tail[(c + e) * B + from + u] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
+    }
+  }
+}
+
+template <int D, int B, int CODE>
+__global__ void __launch_bounds__(256) append_kernel(Cache8 c, const int32_t* __restrict__ cu,
+                                                     const uint16_t* __restrict__ k,
+                                                     const uint16_t* __restrict__ v,
+                                                     int64_t layer_stride, int64_t token_stride,
+                                                     int64_t head_stride) {
+  constexpr int PPR = D / 8, RPP = 256 / PPR;       // pieces of a row, rows of a pass
+  constexpr int N = B >= RPP ? B / RPP : 1;         // passes over a block
+  constexpr int LDT = B + 4;                        // row of the transposed codes in LDS
+  __shared__ uint32_t wave_max[4];
+  __shared__ __align__(16) uint8_t turn[D * LDT];
+  const int row = blockIdx.x, is_v = blockIdx.z;  // row: (layer, sequence, kv head)
+  const int b = row / c.n_kv_heads % c.n_seqs;
+  const Span sp = span_of(cu, c.lens, b, B);
+  const int64_t l = row / c.n_kv_heads / c.n_seqs, h = row % c.n_kv_heads;
+  const uint16_t* src = (is_v ? v : k) + l * layer_stride + h * head_stride + (int64_t)cu[b] * token_stride;
+  uint16_t* tail = (is_v ? c.v_tail : c.k_tail) + (int64_t)row * B * D;
+  // tokens of the last block, when it is not full and not past the table
+  const int rest = sp.end / B <= c.max_blocks ? (int)(sp.end % B) : 0;
+  const bool old = sp.before % B != 0, moves = old && rest != 0 && sp.blocks > 1;
+  const int cc = threadIdx.x % PPR * 8, r0 = threadIdx.x / PPR;
+  for (int i = blockIdx.y; i < sp.blocks; i += gridDim.y) {
+    const int64_t j = sp.j0 + i, t0 = j * B;
+    if (t0 + B <= sp.end) {
+      const int32_t id = j < c.max_blocks ? c.table[(int64_t)row * c.max_blocks + j] : -1;
+      if (id >= 0 && id < c.n_blocks) {
+        uint4 x[N];
+        uint32_t mx = 0;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+          const int u = r0 + n * RPP;
+          x[n] = make_uint4(0, 0, 0, 0);
+          if (u < B) {
+            const int64_t t = t0 + u;
+            if (t >= sp.before) {
+              x[n] = *reinterpret_cast<const uint4*>(src + (t - sp.before) * token_stride + cc);
+            } else if (!is_v) {
+              x[n] = *reinterpret_cast<const uint4*>(tail + u * D + cc);
+            } else {
+              uint32_t w[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                w[e] = tail[(cc + 2 * e) * B + u] | (uint32_t)tail[(cc + 2 * e + 1) * B + u] << 16;
+              x[n] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+          }
+          const uint32_t w[4] = {x[n].x, x[n].y, x[n].z, x[n].w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t lo = w[e] & 0x7FFFu, hi = w[e] >> 16 & 0x7FFFu;
+            mx = max(mx, max(lo, hi));
+          }
+        }
+        for (int m = 32; m > 0; m >>= 1) mx = max(mx, (uint32_t)__shfl_xor((int)mx, m, 64));
+        if ((threadIdx.x & 63) == 0) wave_max[threadIdx.x >> 6] = mx;
+        __syncthreads();
+        mx = max(max(wave_max[0], wave_max[1]), max(wave_max[2], wave_max[3]));
+        const Scale sc = scale_of<CODE>(mx);
+        if (threadIdx.x == 0) (is_v ? c.v_scale : c.k_scale)[id] = sc.scale;
+        const bool none = mx == 0 || mx >= 0x7F80u;  // every code 0
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+          const int u = r0 + n * RPP;
+          if (u >= B) continue;
+          const uint32_t w[4] = {x[n].x, x[n].y, x[n].z, x[n].w};
+          float f[8];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) f[2 * e] = bf16_lo(w[e]), f[2 * e + 1] = bf16_hi(w[e]);
+          uint2 q = make_uint2(0, 0);
+          if (!none) q = make_uint2(codes4<CODE>(f, sc), codes4<CODE>(f + 4, sc));
+          if (!is_v) {
+            *reinterpret_cast<uint2*>(c.k_codes + (int64_t)id * B * D + u * D + cc) = q;
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              turn[(cc + e) * LDT + u] = (uint8_t)((e < 4 ? q.x : q.y) >> (8 * (e & 3)));
+          }
+        }
+        __syncthreads();  // the codes are in LDS, wave_max and the old tail have been read
+        if (is_v) {
+          uint8_t* dst = c.v_codes + (int64_t)id * B * D;
+          for (int p = threadIdx.x; p < D * B / 16; p += 256) {
+            const uint8_t* t = turn + p / (B / 16) * LDT + p % (B / 16) * 16;
+            const uint32_t* w = reinterpret_cast<const uint32_t*>(t);
+            *reinterpret_cast<uint4*>(dst + p * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+          __syncthreads();
+        }
+      }
+      // the workgroup that read the old tail is the one that may write the new one
+      if (i == 0 && moves) {
+        __syncthreads();
+        write_tail<D, B>(is_v, tail, src + (sp.end - rest - sp.before) * token_stride, token_stride, 0, rest);
+      }
+    } else if (rest != 0 && !(moves && i > 0)) {
+      const int from = (int)(sp.before > t0 ? sp.before - t0 : 0);
+      write_tail<D, B>(is_v, tail, src + (t0 + from - sp.before) * token_stride, token_stride, from, rest);
+    }
+  }
+}
+
+// ---- read -----------------------------------------------------------------
+
+__device__ __forceinline__ void store8(float* p, const float* x) {
+  *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+  *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+}
+__device__ __forceinline__ void store8(uint16_t* p, const float* x) {
+  *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]),
+                                            pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+}
+
+template <int D, int B, int CODE, typename T>
+__global__ void __launch_bounds__(256) read_kernel(Cache8 c, const int32_t* __restrict__ cu,
+                                                   T* __restrict__ k, T* __restrict__ v,
+                                                   int64_t layer_stride, int64_t token_stride,
+                                                   int64_t head_stride) {
+  constexpr int PPR = D / 8, LDT = B + 4;
+  __shared__ __align__(16) uint8_t turn[D * LDT];
+  const int row = blockIdx.x, is_v = blockIdx.z;
+  const int b = row / c.n_kv_heads % c.n_seqs;
+  const Span sp = span_of(cu, c.lens, b, B);
+  const int64_t l = row / c.n_kv_heads / c.n_seqs, h = row % c.n_kv_heads;
+  T* dst = (is_v ? v : k) + l * layer_stride + h * head_stride + (int64_t)cu[b] * token_stride;
+  const uint16_t* tail = (is_v ? c.v_tail : c.k_tail) + (int64_t)row * B * D;
+  for (int i = blockIdx.y; i < sp.blocks; i += gridDim.y) {
+    const int64_t j = sp.j0 + i, t0 = j * B;
+    const int from = (int)(sp.before > t0 ? sp.before - t0 : 0);
+    const int to = (int)(sp.end - t0 < B ? sp.end - t0 : B);
+    T* out = dst + (t0 - sp.before) * token_stride;
+    if (t0 + B <= sp.end) {
+      const int32_t id = j < c.max_blocks ? c.table[(int64_t)row * c.max_blocks + j] : -1;
+      if (id < 0 || id >= c.n_blocks) continue;
+      const float scale = (is_v ? c.v_scale : c.k_scale)[id];
+      const uint8_t* codes = (is_v ? c.v_codes : c.k_codes) + (int64_t)id * B * D;
+      if (is_v) {
+        __syncthreads();
+        for (int p = threadIdx.x; p < D * B / 16; p += 256) {
+          const uint4 q = *reinterpret_cast<const uint4*>(codes + p * 16);
+          uint32_t* w = reinterpret_cast<uint32_t*>(turn + p / (B / 16) * LDT + p % (B / 16) * 16);
+          w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
+        }
+        __syncthreads();
+      }
+      for (int p = threadIdx.x + from * PPR; p < to * PPR; p += 256) {
+        const int u = p / PPR, cc = p % PPR * 8;
+        uint32_t q[2] = {0, 0};
+        if (!is_v) {
+          const uint2 w = *reinterpret_cast<const uint2*>(codes + u * D + cc);
+          q[0] = w.x, q[1] = w.y;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) q[e / 4] |= (uint32_t)turn[(cc + e) * LDT + u] << (8 * (e & 3));
+        }
+        float x[8];
+        values4<CODE>(q[0], scale, x);
+        values4<CODE>(q[1], scale, x + 4);
+        store8(out + (int64_t)u * token_stride + cc, x);
+      }
+    } else if (j <= c.max_blocks) {
+      for (int p = threadIdx.x + from * PPR; p < to * PPR; p += 256) {
+        const int u = p / PPR, cc = p % PPR * 8;
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          x[e] = bf16_lo(is_v ? tail[(cc + e) * B + u] : tail[u * D + cc + e]);
+        store8(out + (int64_t)u * token_stride + cc, x);
+      }
+    }
+  }
+}
+
+// ---- evict ----------------------------------------------------------------
+
+// float -> unsigned key of the same order: NaN lowest, -0 equal to +0
+__device__ __forceinline__ uint32_t order_key(float x) {
+  const uint32_t u = __float_as_uint(x + 0.f);
+  if ((u & 0x7FFFFFFFu) > 0x7F800000u) return 0;
+  return (u & 0x80000000u) ? ~u : u | 0x80000000u;
+}
+
+// One workgroup per table row.  The k-th largest key of the middle blocks is found
+// digit by digit (8 bits) from counts in LDS; the row is then written in order with
+// the ranks of kept and dropped entries from ballots.  Counts decide, so the result
+// does not depend on the order of the atomics.
+__global__ void __launch_bounds__(256) evict_kernel(Evict a) {
+  __shared__ int32_t bins[256], wave_kept[4], wave_ties[4];
+  __shared__ uint32_t s_prefix;
+  __shared__ int32_t s_left;
+  const int64_t row = blockIdx.x;
+  const int b = (int)(row / a.n_kv_heads % a.n_seqs);
+  const int M = a.max_blocks, tid = threadIdx.x;
+  const int32_t* table = a.table + row * M;
+  const float* weights = a.weights + row * M;
+  int32_t* table_out = a.table_out + row * M;
+  float* weights_out = a.weights_out + row * M;
+  const int32_t len = max(a.lens[b], 0);
+  const int nb = min(len / a.block_len, M);
+  const int drop = nb > a.budget ? nb - a.budget : 0;
+  if (row / a.n_kv_heads < a.n_seqs && row % a.n_kv_heads == 0 && tid == 0)
+    a.lens_out[b] = a.lens[b] - drop * a.block_len;
+  if (drop == 0) {
+    for (int i = tid; i < M; i += 256) table_out[i] = table[i], weights_out[i] = weights[i];
+    return;
+  }
+  const int lo = a.n_first, hi = nb - a.n_recent;  // the blocks that compete
+  const int k = a.budget - a.n_first - a.n_recent;
+  uint32_t prefix = 0;
+  int left = k;  // of the keys that start with prefix, the `left` largest are kept
+  if (k > 0) {
+    for (int shift = 24; shift >= 0; shift -= 8) {
+      bins[tid] = 0;
+      __syncthreads();
+      for (int i = lo + tid; i < hi; i += 256) {
+        const uint32_t key = order_key(weights[i]);
+        if (shift == 24 || key >> (shift + 8) == prefix >> (shift + 8))
+          atomicAdd(&bins[key >> shift & 255], 1);
+      }
+      __syncthreads();
+      if (tid == 0) {
+        int above = 0, d = 255;
+        while (d > 0 && above + bins[d] < left) above += bins[d--];
+        s_prefix = prefix | (uint32_t)d << shift;
+        s_left = left - above;
+      }
+      __syncthreads();
+      prefix = s_prefix;
+      left = s_left;
+    }
+  }
+  // kept: forced, above the k-th key, or among the first `left` equal to it
+  int kept_before = 0, ties_before = 0;
+  for (int base = 0; base < nb; base += 256) {
+    const int i = base + tid;
+    const bool in = i < nb, middle = in && i >= lo && i < hi;
+    const float w = in ? weights[i] : 0.f;
+    const uint32_t key = order_key(w);
+    const bool tie = middle && k > 0 && key == prefix;
+    const uint64_t tm = __ballot(tie), below = (1ull << (tid & 63)) - 1;
+    if ((tid & 63) == 0) wave_ties[tid >> 6] = __popcll(tm);
+    __syncthreads();
+    int ties = ties_before + __popcll(tm & below);
+    for (int q = 0; q < 4; ++q) {
+      if (q < tid >> 6) ties += wave_ties[q];
+      ties_before += wave_ties[q];
+    }
+    const bool keep = in && (!middle || (k > 0 && (key > prefix || (tie && ties < left))));
+    const uint64_t km = __ballot(keep);
+    if ((tid & 63) == 0) wave_kept[tid >> 6] = __popcll(km);
+    __syncthreads();
+    int kept = kept_before + __popcll(km & below);
+    for (int q = 0; q < 4; ++q) {
+      if (q < tid >> 6) kept += wave_kept[q];
+      kept_before += wave_kept[q];
+    }
+    if (in) {
+      const int to = keep ? kept : M - drop + (i - kept);
+      table_out[to] = table[i];
+      weights_out[to] = keep ? w : 0.f;
+    }
+    __syncthreads();
+  }
+  for (int i = nb + tid; i < M; i += 256) {
+    table_out[i - drop] = table[i];
+    weights_out[i - drop] = weights[i];
+  }
+}
+
+template <int D, int B>
+void append(const Cache8& c, int code, dim3 grid, hipStream_t s, const int32_t* cu, const uint16_t* k,
+            const uint16_t* v, int64_t ls, int64_t ts, int64_t hs) {
+  if (code == KVB_I8)
+    hipLaunchKernelGGL((append_kernel<D, B, KVB_I8>), grid, dim3(256), 0, s, c, cu, k, v, ls, ts, hs);
+  else
+    hipLaunchKernelGGL((append_kernel<D, B, KVB_E4M3>), grid, dim3(256), 0, s, c, cu, k, v, ls, ts, hs);
+}
+
+template <int D, int B>
+void read(const Cache8& c, int code, kvb_dtype dtype, dim3 grid, hipStream_t s, const int32_t* cu, void* k,
+          void* v, int64_t ls, int64_t ts, int64_t hs) {
+#define KVB_READ(C, T)                                                                          \
+  hipLaunchKernelGGL((read_kernel<D, B, C, T>), grid, dim3(256), 0, s, c, cu, (T*)k, (T*)v, ls, \
+                     ts, hs)
+  if (code == KVB_I8) {
+    if (dtype == KVB_BF16) KVB_READ(KVB_I8, uint16_t);
+    else KVB_READ(KVB_I8, float);
+  } else {
+    if (dtype == KVB_BF16) KVB_READ(KVB_E4M3, uint16_t);
+    else KVB_READ(KVB_E4M3, float);
+  }
+#undef KVB_READ
+}
+
+// blocks that n consecutive tokens can touch
+dim3 span_grid(const Cache8& c, int n_layers, int B, int n) {
+  const int64_t blocks = ((int64_t)n + B - 2) / B + 1;
+  return dim3((unsigned)((int64_t)n_layers * c.n_seqs * c.n_kv_heads),
+              (unsigned)(blocks < 65535 ? blocks : 65535), 2);
+}
+
+}  // namespace
+
+#define KVB_FOR_LAYOUT(F, ...)                     \
+  do {                                             \
+    if (head_dim == 128) {                         \
+      if (block_len == 16) F<128, 16>(__VA_ARGS__); \
+      else if (block_len == 32) F<128, 32>(__VA_ARGS__); \
+      else if (block_len == 64) F<128, 64>(__VA_ARGS__); \
+      else F<128, 128>(__VA_ARGS__);               \
+    } else {                                       \
+      if (block_len == 16) F<64, 16>(__VA_ARGS__);  \
+      else if (block_len == 32) F<64, 32>(__VA_ARGS__); \
+      else if (block_len == 64) F<64, 64>(__VA_ARGS__); \
+      else F<64, 128>(__VA_ARGS__);                \
+    }                                              \
+  } while (0)
+
+hipError_t launch_cache8_append(const Cache8& c, int head_dim, int block_len, int code, int n_layers,
+                                const int32_t* cu_new, int max_new, const uint16_t* k,
+                                const uint16_t* v, int64_t layer_stride, int64_t token_stride,
+                                int64_t head_stride, hipStream_t s) {
+  const dim3 grid = span_grid(c, n_layers, block_len, max_new);
+  KVB_FOR_LAYOUT(append, c, code, grid, s, cu_new, k, v, layer_stride, token_stride, head_stride);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache8_read(const Cache8& c, int head_dim, int block_len, int code, int n_layers,
+                              const int32_t* cu_out, int max_out, kvb_dtype dtype, void* k, void* v,
+                              int64_t layer_stride, int64_t token_stride, int64_t head_stride,
+                              hipStream_t s) {
+  const dim3 grid = span_grid(c, n_layers, block_len, max_out);
+  KVB_FOR_LAYOUT(read, c, code, dtype, grid, s, cu_out, k, v, layer_stride, token_stride, head_stride);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache8_evict(const Evict& a, int n_layers, hipStream_t s) {
+  const int64_t rows = (int64_t)n_layers * a.n_seqs * a.n_kv_heads;
+  hipLaunchKernelGGL(evict_kernel, dim3((unsigned)rows), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace kvb

@@ -564,4 +564,284 @@ kvb_status kvb_sparse_attn(int32_t n_layers, int32_t n_q_heads, int32_t n_kv_hea
                     "kvb_sparse_attn");
 }
 
+// ---- decoding ----------------------------------------------------------------
+
+kvb_status kvb_rope_scaled_table(double theta, int32_t rot_dim, const kvb_rope_scaling* scaling,
+                                 const int32_t* pos, int32_t n, float* cos_out, float* sin_out) {
+  REQUIRE(n >= 0, "n < 0");
+  REQUIRE(rot_dim > 0 && rot_dim % 2 == 0, "rot_dim %d must be even and positive", rot_dim);
+  REQUIRE(theta > 0.0 && isfinite(theta), "theta must be positive");
+  kvb_rope_scaling sc = {KVB_ROPE_NONE, 1.0, 1.0, 1.0, 2.0, 1.0};
+  if (scaling) sc = *scaling;
+  REQUIRE(sc.kind >= KVB_ROPE_NONE && sc.kind <= KVB_ROPE_INDEX, "unknown scaling %d", sc.kind);
+  REQUIRE(sc.attn_factor > 0.0 && isfinite(sc.attn_factor), "attn_factor must be positive");
+  if (sc.kind != KVB_ROPE_NONE)
+    REQUIRE(sc.factor >= 1.0 && isfinite(sc.factor), "factor must be at least 1");
+  if (sc.kind == KVB_ROPE_NTK) REQUIRE(rot_dim > 2, "NTK scaling needs rot_dim > 2");
+  if (sc.kind == KVB_ROPE_PARTS || sc.kind == KVB_ROPE_INDEX) {
+    REQUIRE(sc.original_len > 0.0 && isfinite(sc.original_len), "original_len must be positive");
+    REQUIRE(sc.low > 0.0 && sc.high > sc.low && isfinite(sc.high), "need 0 < low < high");
+  }
+  if (sc.kind == KVB_ROPE_INDEX) REQUIRE(theta > 1.0, "INDEX scaling needs theta > 1");
+  if (n == 0) return ok();
+  REQUIRE_PTR(pos);
+  REQUIRE_PTR(cos_out);
+  REQUIRE_PTR(sin_out);
+  const int half = rot_dim / 2;
+  const double two_pi = 2.0 * M_PI;
+  if (sc.kind == KVB_ROPE_NTK) theta *= pow(sc.factor, rot_dim / (rot_dim - 2.0));
+  double i0 = 0.0, i1 = 1.0;
+  if (sc.kind == KVB_ROPE_INDEX) {
+    i0 = fmax(floor(half * log(sc.original_len / (two_pi * sc.high)) / log(theta)), 0.0);
+    i1 = fmin(ceil(half * log(sc.original_len / (two_pi * sc.low)) / log(theta)), rot_dim - 1.0);
+  }
+  std::vector<double> w(half);
+  for (int i = 0; i < half; ++i) {
+    w[i] = pow(theta, -(2.0 * i) / rot_dim);
+    if (sc.kind == KVB_ROPE_LINEAR) {
+      w[i] /= sc.factor;
+    } else if (sc.kind == KVB_ROPE_PARTS) {
+      const double r = sc.original_len * w[i] / two_pi;
+      const double g = fmin(fmax((r - sc.low) / (sc.high - sc.low), 0.0), 1.0);
+      w[i] = g * w[i] + (1.0 - g) * w[i] / sc.factor;
+    } else if (sc.kind == KVB_ROPE_INDEX) {
+      const double h = fmin(fmax((i - i0) / fmax(i1 - i0, 0.001), 0.0), 1.0);
+      w[i] = (1.0 - h) * w[i] + h * w[i] / sc.factor;
+    }
+  }
+  for (int32_t k = 0; k < n; ++k) {
+    for (int i = 0; i < half; ++i) {
+      const double a = (double)pos[k] * w[i];
+      cos_out[(size_t)k * half + i] = (float)(cos(a) * sc.attn_factor);
+      sin_out[(size_t)k * half + i] = (float)(sin(a) * sc.attn_factor);
+    }
+  }
+  return ok();
+}
+
+kvb_status kvb_qk_norm_rope(int64_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads,
+                            int32_t head_dim, kvb_dtype dtype, const void* q,
+                            int64_t q_token_stride, int64_t q_head_stride, const void* k,
+                            int64_t k_token_stride, int64_t k_head_stride, const float* q_weight,
+                            const float* k_weight, float eps, const int32_t* pos,
+                            const float* table_cos, const float* table_sin, int32_t table_len,
+                            int32_t rot_dim, kvb_pairing pairing, void* q_out,
+                            int64_t q_out_token_stride, int64_t q_out_head_stride, void* k_out,
+                            int64_t k_out_token_stride, int64_t k_out_head_stride, void* stream) {
+  REQUIRE(n_tokens > 0 && n_tokens <= INT32_MAX, "n_tokens must be in (0, 2^31)");
+  REQUIRE(n_q_heads >= 0 && n_kv_heads >= 0 && n_q_heads + (int64_t)n_kv_heads > 0,
+          "head counts must be non-negative, one of them positive");
+  REQUIRE(head_dim > 0 && rot_dim >= 0 && rot_dim <= head_dim,
+          "head_dim must be positive and rot_dim in [0, head_dim]");
+  if (head_dim % 8 != 0 || head_dim > 256 || rot_dim % 8 != 0)
+    return fail(KVB_EUNSUPPORTED, "head_dim %d, rot_dim %d: multiples of 8 up to 256", head_dim,
+                rot_dim);
+  REQUIRE(n_tokens * (n_q_heads + (int64_t)n_kv_heads) <= (int64_t)1 << 30,
+          "too many heads: n_tokens * (n_q_heads + n_kv_heads) > 2^30");
+  REQUIRE(dtype == KVB_BF16 || dtype == KVB_F32, "dtype must be BF16 or F32");
+  REQUIRE(pairing == KVB_PAIR_HALF || pairing == KVB_PAIR_INTERLEAVED, "unknown pairing %d",
+          (int)pairing);
+  REQUIRE(eps >= 0.0f, "eps must not be negative");
+  if (n_q_heads > 0) {
+    REQUIRE(q != nullptr && q_out != nullptr && aligned16(q) && aligned16(q_out),
+            "null or misaligned queries");
+    REQUIRE(q_weight == nullptr || aligned16(q_weight), "q_weight is not 16-byte aligned");
+  }
+  if (n_kv_heads > 0) {
+    REQUIRE(k != nullptr && k_out != nullptr && aligned16(k) && aligned16(k_out),
+            "null or misaligned keys");
+    REQUIRE(k_weight == nullptr || aligned16(k_weight), "k_weight is not 16-byte aligned");
+  }
+  const int64_t strides[] = {q_token_stride,     q_head_stride,     k_token_stride,
+                             k_head_stride,      q_out_token_stride, q_out_head_stride,
+                             k_out_token_stride, k_out_head_stride};
+  for (int64_t x : strides) REQUIRE(x >= 0 && x % 8 == 0, "strides must be multiples of 8");
+  if (rot_dim > 0) {
+    REQUIRE_PTR(pos);
+    REQUIRE_PTR(table_cos);
+    REQUIRE_PTR(table_sin);
+    REQUIRE_ALIGNED(table_cos);
+    REQUIRE_ALIGNED(table_sin);
+    REQUIRE(table_len > 0, "table_len must be positive");
+  }
+  kvb::QkNormRope a{};
+  a.n_tokens = n_tokens;
+  a.n_q_heads = n_q_heads, a.n_kv_heads = n_kv_heads, a.head_dim = head_dim;
+  a.rot_dim = rot_dim, a.pairing = pairing, a.table_len = table_len, a.eps = eps;
+  a.q = q, a.k = k, a.q_weight = q_weight, a.k_weight = k_weight;
+  a.table_cos = table_cos, a.table_sin = table_sin, a.pos = pos;
+  a.q_out = q_out, a.k_out = k_out;
+  a.q_token_stride = q_token_stride, a.q_head_stride = q_head_stride;
+  a.k_token_stride = k_token_stride, a.k_head_stride = k_head_stride;
+  a.q_out_token_stride = q_out_token_stride, a.q_out_head_stride = q_out_head_stride;
+  a.k_out_token_stride = k_out_token_stride, a.k_out_head_stride = k_out_head_stride;
+  return hip_status(kvb::launch_qk_norm_rope(a, dtype, (hipStream_t)stream), "kvb_qk_norm_rope");
+}
+
+static kvb_status check_cache8(const kvb_cache8_layout* p, bool table_only = false) {
+  REQUIRE(p != nullptr, "layout is NULL");
+  REQUIRE(p->n_kv_heads > 0 && p->block_len > 0 && p->max_blocks > 0,
+          "cache layout has a non-positive size");
+  if (table_only) return KVB_OK;
+  REQUIRE(p->n_blocks > 0 && p->head_dim > 0, "cache layout has a non-positive size");
+  if (kvb_status s = check_head_dim(p->head_dim)) return s;
+  if (p->block_len != 16 && p->block_len != 32 && p->block_len != 64 && p->block_len != 128)
+    return fail(KVB_EUNSUPPORTED, "block_len %d: built for 16, 32, 64 and 128", p->block_len);
+  REQUIRE(p->code == KVB_I8 || p->code == KVB_E4M3, "unknown code %d", p->code);
+  return KVB_OK;
+}
+
+static kvb_status check_cache8_rows(const kvb_cache8_layout* p, int32_t n_layers, int32_t n_seqs) {
+  REQUIRE(n_layers > 0 && n_seqs > 0, "n_layers and n_seqs must be positive");
+  REQUIRE(n_layers <= (1 << 20) && n_seqs <= (1 << 20) &&
+              (int64_t)n_layers * n_seqs <= (1 << 23) / p->n_kv_heads,
+          "n_layers * n_seqs * n_kv_heads > 2^23");
+  return KVB_OK;
+}
+
+static kvb_status check_cache8_arrays(const void* const* ptrs, int n) {
+  for (int i = 0; i < n; ++i)
+    REQUIRE(ptrs[i] != nullptr && aligned16(ptrs[i]), "null or misaligned tensor");
+  return KVB_OK;
+}
+
+static kvb::Cache8 cache8_of(const kvb_cache8_layout* p, int32_t n_seqs, const int32_t* table,
+                             const int32_t* lens, const uint8_t* k_codes, const float* k_scale,
+                             const uint8_t* v_codes, const float* v_scale, const uint16_t* k_tail,
+                             const uint16_t* v_tail) {
+  kvb::Cache8 c{};
+  c.n_blocks = p->n_blocks, c.n_kv_heads = p->n_kv_heads, c.n_seqs = n_seqs;
+  c.max_blocks = p->max_blocks;
+  c.table = table, c.lens = lens;
+  c.k_codes = const_cast<uint8_t*>(k_codes), c.v_codes = const_cast<uint8_t*>(v_codes);
+  c.k_scale = const_cast<float*>(k_scale), c.v_scale = const_cast<float*>(v_scale);
+  c.k_tail = const_cast<uint16_t*>(k_tail), c.v_tail = const_cast<uint16_t*>(v_tail);
+  return c;
+}
+
+kvb_status kvb_cache8_append(const kvb_cache8_layout* layout, int32_t n_layers, int32_t n_seqs,
+                             const int32_t* cu_new, int32_t max_new, const uint16_t* k,
+                             const uint16_t* v, int64_t layer_stride, int64_t token_stride,
+                             int64_t head_stride, const int32_t* table, const int32_t* lens,
+                             uint8_t* k_codes, float* k_scale, uint8_t* v_codes, float* v_scale,
+                             uint16_t* k_tail, uint16_t* v_tail, void* stream) {
+  if (kvb_status s = check_cache8(layout)) return s;
+  if (kvb_status s = check_cache8_rows(layout, n_layers, n_seqs)) return s;
+  REQUIRE(max_new > 0, "max_new must be positive");
+  const int64_t strides[] = {layer_stride, token_stride, head_stride};
+  for (int64_t x : strides) REQUIRE(x >= 0 && x % 8 == 0, "strides must be multiples of 8");
+  REQUIRE(cu_new != nullptr && table != nullptr && lens != nullptr, "a required pointer is NULL");
+  const void* ptrs[] = {k, v, k_codes, k_scale, v_codes, v_scale, k_tail, v_tail};
+  if (kvb_status s = check_cache8_arrays(ptrs, 8)) return s;
+  return hip_status(
+      kvb::launch_cache8_append(cache8_of(layout, n_seqs, table, lens, k_codes, k_scale, v_codes,
+                                          v_scale, k_tail, v_tail),
+                                layout->head_dim, layout->block_len, layout->code, n_layers, cu_new,
+                                max_new, k, v, layer_stride, token_stride, head_stride,
+                                (hipStream_t)stream),
+      "kvb_cache8_append");
+}
+
+kvb_status kvb_cache8_read(const kvb_cache8_layout* layout, int32_t n_layers, int32_t n_seqs,
+                           const int32_t* cu_out, int32_t max_out, const int32_t* table,
+                           const int32_t* lens, const uint8_t* k_codes, const float* k_scale,
+                           const uint8_t* v_codes, const float* v_scale, const uint16_t* k_tail,
+                           const uint16_t* v_tail, kvb_dtype out_dtype, void* k_out, void* v_out,
+                           int64_t layer_stride, int64_t token_stride, int64_t head_stride,
+                           void* stream) {
+  if (kvb_status s = check_cache8(layout)) return s;
+  if (kvb_status s = check_cache8_rows(layout, n_layers, n_seqs)) return s;
+  REQUIRE(max_out > 0, "max_out must be positive");
+  REQUIRE(out_dtype == KVB_BF16 || out_dtype == KVB_F32, "out_dtype must be BF16 or F32");
+  const int64_t strides[] = {layer_stride, token_stride, head_stride};
+  for (int64_t x : strides) REQUIRE(x >= 0 && x % 8 == 0, "strides must be multiples of 8");
+  REQUIRE(cu_out != nullptr && table != nullptr && lens != nullptr, "a required pointer is NULL");
+  const void* ptrs[] = {k_out, v_out, k_codes, k_scale, v_codes, v_scale, k_tail, v_tail};
+  if (kvb_status s = check_cache8_arrays(ptrs, 8)) return s;
+  return hip_status(
+      kvb::launch_cache8_read(cache8_of(layout, n_seqs, table, lens, k_codes, k_scale, v_codes,
+                                        v_scale, k_tail, v_tail),
+                              layout->head_dim, layout->block_len, layout->code, n_layers, cu_out,
+                              max_out, out_dtype, k_out, v_out, layer_stride, token_stride,
+                              head_stride, (hipStream_t)stream),
+      "kvb_cache8_read");
+}
+
+// Sizes of an attention call; KVB_OK when the plan can be made.
+static kvb_status check_cache8_attn(const kvb_cache8_layout* p, int32_t n_q_heads, int32_t n_seqs,
+                                    int32_t n_queries, int32_t max_queries, int32_t max_len) {
+  if (kvb_status s = check_cache8(p)) return s;
+  REQUIRE(n_q_heads > 0 && n_q_heads % p->n_kv_heads == 0,
+          "n_q_heads %d is not a multiple of n_kv_heads %d", n_q_heads, p->n_kv_heads);
+  REQUIRE(n_seqs > 0 && (int64_t)n_seqs * p->n_kv_heads <= 65535,
+          "n_seqs * n_kv_heads must be in [1, 65535]");
+  REQUIRE(n_queries > 0 && max_queries > 0 && max_len > 0,
+          "n_queries, max_queries and max_len must be positive");
+  REQUIRE((int64_t)max_queries * (n_q_heads / p->n_kv_heads) <= (1 << 20),
+          "max_queries * (n_q_heads / n_kv_heads) > 2^20");
+  return KVB_OK;
+}
+
+size_t kvb_cache8_attn_workspace_bytes(const kvb_cache8_layout* layout, int32_t n_q_heads,
+                                       int32_t n_seqs, int32_t n_queries, int32_t max_queries,
+                                       int32_t max_len, int32_t with_weights) {
+  if (check_cache8_attn(layout, n_q_heads, n_seqs, n_queries, max_queries, max_len) != KVB_OK) return 0;
+  return kvb::attn8_plan(layout->n_kv_heads, layout->head_dim, layout->block_len, layout->max_blocks,
+                         n_q_heads, n_seqs, max_queries, max_len, with_weights != 0)
+      .workspace;
+}
+
+kvb_status kvb_cache8_attn(const kvb_cache8_layout* layout, int32_t n_q_heads, int32_t n_seqs,
+                           const int32_t* cu_q, int32_t n_queries, int32_t max_queries,
+                           int32_t max_len, const uint16_t* q, const int32_t* table,
+                           const int32_t* lens, const uint8_t* k_codes, const float* k_scale,
+                           const uint8_t* v_codes, const float* v_scale, const uint16_t* k_tail,
+                           const uint16_t* v_tail, float softmax_scale, uint16_t* out, float* lse,
+                           const float* weights_in, float* weights_out, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+  if (kvb_status s = check_cache8_attn(layout, n_q_heads, n_seqs, n_queries, max_queries, max_len))
+    return s;
+  REQUIRE(cu_q != nullptr && table != nullptr && lens != nullptr, "a required pointer is NULL");
+  const void* ptrs[] = {q, out, k_codes, k_scale, v_codes, v_scale, k_tail, v_tail};
+  if (kvb_status s = check_cache8_arrays(ptrs, 8)) return s;
+  REQUIRE(weights_out != nullptr || weights_in == nullptr, "weights_in without weights_out");
+  REQUIRE(isfinite(softmax_scale), "softmax_scale must be finite");
+  const kvb::Attn8Plan plan =
+      kvb::attn8_plan(layout->n_kv_heads, layout->head_dim, layout->block_len, layout->max_blocks,
+                      n_q_heads, n_seqs, max_queries, max_len, weights_out != nullptr);
+  REQUIRE(workspace_bytes >= plan.workspace, "workspace %zu bytes, need %zu", workspace_bytes,
+          plan.workspace);
+  if (plan.workspace)
+    REQUIRE(workspace != nullptr && aligned16(workspace), "workspace NULL or misaligned");
+  kvb::Attn8 a{};
+  a.c = cache8_of(layout, n_seqs, table, lens, k_codes, k_scale, v_codes, v_scale, k_tail, v_tail);
+  a.n_q_heads = n_q_heads, a.n_queries = n_queries;
+  a.cu_q = cu_q, a.q = q, a.out = out, a.lse = lse, a.softmax_scale = softmax_scale;
+  a.weights_in = weights_in, a.weights_out = weights_out;
+  return hip_status(kvb::launch_cache8_attn(plan, a, layout->head_dim, layout->block_len,
+                                            layout->code, workspace, (hipStream_t)stream),
+                    "kvb_cache8_attn");
+}
+
+kvb_status kvb_cache8_evict(const kvb_cache8_layout* layout, int32_t n_layers, int32_t n_seqs,
+                            int32_t budget, int32_t n_first, int32_t n_recent,
+                            const int32_t* table, const int32_t* lens, const float* weights,
+                            int32_t* table_out, int32_t* lens_out, float* weights_out,
+                            void* stream) {
+  if (kvb_status s = check_cache8(layout, true)) return s;
+  if (kvb_status s = check_cache8_rows(layout, n_layers, n_seqs)) return s;
+  REQUIRE(n_first >= 0 && n_recent >= 0 && (int64_t)n_first + n_recent <= budget,
+          "n_first and n_recent must be non-negative and fit the budget");
+  const void* ptrs[] = {table, lens, weights, table_out, lens_out, weights_out};
+  for (const void* p : ptrs) REQUIRE(p != nullptr, "a required pointer is NULL");
+  REQUIRE(table != table_out && lens != lens_out && weights != weights_out,
+          "an output is an input");
+  kvb::Evict a{};
+  a.n_seqs = n_seqs, a.n_kv_heads = layout->n_kv_heads, a.block_len = layout->block_len;
+  a.max_blocks = layout->max_blocks, a.budget = budget, a.n_first = n_first, a.n_recent = n_recent;
+  a.table = table, a.lens = lens, a.weights = weights;
+  a.table_out = table_out, a.lens_out = lens_out, a.weights_out = weights_out;
+  return hip_status(kvb::launch_cache8_evict(a, n_layers, (hipStream_t)stream), "kvb_cache8_evict");
+}
+
 }  // extern "C"

@@ -111,4 +111,72 @@ hipError_t launch_sparse_attn_layer(const AttnPlan& layer_plan, int layer, int n
                                     const void* plans, float softmax_scale, kvb_dtype out_dtype,
                                     void* out, void* workspace, hipStream_t s);
 
+// ---- decoding ---------------------------------------------------------------
+struct QkNormRope {
+  int64_t n_tokens;
+  int32_t n_q_heads, n_kv_heads, head_dim, rot_dim, pairing, table_len;
+  int32_t chunks;  // waves per token (set by the launcher)
+  float eps;
+  const void *q, *k;
+  const float *q_weight, *k_weight, *table_cos, *table_sin;
+  const int32_t* pos;
+  void *q_out, *k_out;
+  int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride;
+  int64_t q_out_token_stride, q_out_head_stride, k_out_token_stride, k_out_head_stride;
+};
+hipError_t launch_qk_norm_rope(const QkNormRope& a, kvb_dtype dtype, hipStream_t s);
+
+struct Cache8 {
+  int32_t n_blocks, n_kv_heads, n_seqs, max_blocks;
+  const int32_t *table, *lens;
+  uint8_t *k_codes, *v_codes;
+  float *k_scale, *v_scale;
+  uint16_t *k_tail, *v_tail;
+};
+hipError_t launch_cache8_append(const Cache8& c, int head_dim, int block_len, int code, int n_layers,
+                                const int32_t* cu_new, int max_new, const uint16_t* k,
+                                const uint16_t* v, int64_t layer_stride, int64_t token_stride,
+                                int64_t head_stride, hipStream_t s);
+// only reads the cache
+hipError_t launch_cache8_read(const Cache8& c, int head_dim, int block_len, int code, int n_layers,
+                              const int32_t* cu_out, int max_out, kvb_dtype dtype, void* k, void* v,
+                              int64_t layer_stride, int64_t token_stride, int64_t head_stride,
+                              hipStream_t s);
+
+struct Evict {
+  int32_t n_seqs, n_kv_heads, block_len, max_blocks, budget, n_first, n_recent;
+  const int32_t *table, *lens;
+  const float* weights;
+  int32_t *table_out, *lens_out;
+  float* weights_out;
+};
+hipError_t launch_cache8_evict(const Evict& a, int n_layers, hipStream_t s);
+
+// How a kvb_cache8_attn call is cut into workgroups, and its workspace.
+struct Attn8Plan {
+  int col_tiles;       // 16-query tiles of a wave (1 or 2)
+  int n_tiles;         // query tiles per (sequence, kv head)
+  int n_splits;        // workgroups that share a tile's keys
+  int span;            // 64-key steps of each but the last
+  int64_t rows;        // query rows of a (sequence, kv head), at most
+  int64_t n_parts;     // parts of up to 64 tokens of a block with a weight of their own
+  size_t ml_offset;    // (max, sum) of each (sequence, kv head, split, row)
+  size_t parts_offset; // log2 weight of each (sequence, kv head, part, row)
+  size_t workspace;    // total bytes
+};
+Attn8Plan attn8_plan(int n_kv_heads, int head_dim, int block_len, int max_blocks, int n_q_heads,
+                     int n_seqs, int max_queries, int max_len, bool with_weights);
+struct Attn8 {
+  Cache8 c;
+  int32_t n_q_heads, n_queries;
+  const int32_t* cu_q;
+  const uint16_t* q;
+  uint16_t* out;
+  float *lse, softmax_scale;
+  const float* weights_in;
+  float* weights_out;
+};
+hipError_t launch_cache8_attn(const Attn8Plan& plan, const Attn8& a, int head_dim, int block_len,
+                              int code, void* workspace, hipStream_t s);
+
 }  // namespace kvb

@@ -16,6 +16,9 @@ LIB_PATH = os.path.join(_HERE, "lib", "libkvb.so")
 KVB_OK, KVB_EINVAL, KVB_EUNSUPPORTED, KVB_EHIP = 0, 1, 2, 3
 KVB_BF16, KVB_F32, KVB_F64 = 0, 1, 2
 KVB_ROW_CANDIDATE, KVB_ROW_FORCED = 1, 2
+KVB_ROPE_NONE, KVB_ROPE_LINEAR, KVB_ROPE_NTK, KVB_ROPE_PARTS, KVB_ROPE_INDEX = range(5)
+KVB_PAIR_HALF, KVB_PAIR_INTERLEAVED = 0, 1
+KVB_I8, KVB_E4M3 = 0, 1
 
 _STATUS = {0: "KVB_OK", 1: "KVB_EINVAL", 2: "KVB_EUNSUPPORTED", 3: "KVB_EHIP"}
 
@@ -34,6 +37,16 @@ class kvb_pool_layout(ctypes.Structure):
 
 class kvb_chunk(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("pool_idx", "src_pos", "dst_row", "dst_pos")]
+
+
+class kvb_rope_scaling(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32)] + [(n, ctypes.c_double) for n in
+                                             ("factor", "original_len", "low", "high", "attn_factor")]
+
+
+class kvb_cache8_layout(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("n_blocks", "n_kv_heads", "head_dim", "block_len", "code", "max_blocks")]
 
 
 _i32, _i64, _f32, _f64, _vp, _sz = (ctypes.c_int32, ctypes.c_int64, ctypes.c_float,
@@ -73,6 +86,24 @@ _SIGS = {
     "kvb_sparse_attn_layer": (_i32, [_i32, _i32, _i32, _i32, _i32, _i64, _vp, _i32, _i32, _vp,
                                      _vp, _i32, _i32, _vp, _vp, _vp, _vp, _sz, _f32, _i32, _vp,
                                      _vp, _sz, _vp]),
+    "kvb_rope_scaled_table": (_i32, [_f64, _i32, ctypes.POINTER(kvb_rope_scaling), _vp, _i32, _vp,
+                                     _vp]),
+    "kvb_qk_norm_rope": (_i32, [_i64, _i32, _i32, _i32, _i32, _vp, _i64, _i64, _vp, _i64, _i64,
+                                _vp, _vp, _f32, _vp, _vp, _vp, _i32, _i32, _i32, _vp, _i64, _i64,
+                                _vp, _i64, _i64, _vp]),
+    "kvb_cache8_append": (_i32, [ctypes.POINTER(kvb_cache8_layout), _i32, _i32, _vp, _i32, _vp,
+                                 _vp, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
+                                 _vp]),
+    "kvb_cache8_read": (_i32, [ctypes.POINTER(kvb_cache8_layout), _i32, _i32, _vp, _i32, _vp, _vp,
+                               _vp, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _i64, _i64, _i64,
+                               _vp]),
+    "kvb_cache8_attn_workspace_bytes": (_sz, [ctypes.POINTER(kvb_cache8_layout), _i32, _i32, _i32,
+                                              _i32, _i32, _i32]),
+    "kvb_cache8_attn": (_i32, [ctypes.POINTER(kvb_cache8_layout), _i32, _i32, _vp, _i32, _i32,
+                               _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _f32, _vp, _vp,
+                               _vp, _vp, _vp, _sz, _vp]),
+    "kvb_cache8_evict": (_i32, [ctypes.POINTER(kvb_cache8_layout), _i32, _i32, _i32, _i32, _i32,
+                                _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
 }
 
 
@@ -130,6 +161,14 @@ def _stream(stream):
 
 def pool_layout(n_layers, n_kv_heads, head_dim, bits, k_group, v_group, chunk_len=128):
     return kvb_pool_layout(n_layers, n_kv_heads, head_dim, chunk_len, bits, k_group, v_group)
+
+
+def cache8_layout(n_blocks, n_kv_heads, head_dim, block_len, code, max_blocks):
+    return kvb_cache8_layout(n_blocks, n_kv_heads, head_dim, block_len, code, max_blocks)
+
+
+def rope_scaling(kind, factor=1.0, original_len=1.0, low=1.0, high=32.0, attn_factor=1.0):
+    return kvb_rope_scaling(kind, factor, original_len, low, high, attn_factor)
 
 
 # ---- host helpers -------------------------------------------------------------
@@ -291,3 +330,71 @@ def kvb_sparse_attn_layer(layer, n_layers, n_q_heads, n_kv_heads, head_dim, t_to
                                       _p(v_cache_f16), _p(plans), plans_bytes,
                                       float(softmax_scale), out_dtype, _p(out), _p(workspace),
                                       workspace_bytes, _stream(stream)))
+
+
+# ---- decoding -------------------------------------------------------------------
+
+def kvb_rope_scaled_table(theta: float, rot_dim: int, scaling, pos):
+    pos = np.ascontiguousarray(pos, dtype=np.int32).reshape(-1)
+    n = pos.shape[0]
+    c = np.empty((n, rot_dim // 2), np.float32)
+    s = np.empty((n, rot_dim // 2), np.float32)
+    _check(_lib.kvb_rope_scaled_table(theta, rot_dim,
+                                      None if scaling is None else ctypes.byref(scaling), _p(pos),
+                                      n, _p(c), _p(s)))
+    return c, s
+
+
+def kvb_qk_norm_rope(n_tokens, n_q_heads, n_kv_heads, head_dim, dtype, q, q_token_stride,
+                     q_head_stride, k, k_token_stride, k_head_stride, q_weight, k_weight, eps,
+                     pos, table_cos, table_sin, table_len, rot_dim, pairing, q_out,
+                     q_out_token_stride, q_out_head_stride, k_out, k_out_token_stride,
+                     k_out_head_stride, stream=None):
+    _check(_lib.kvb_qk_norm_rope(n_tokens, n_q_heads, n_kv_heads, head_dim, dtype, _p(q),
+                                 q_token_stride, q_head_stride, _p(k), k_token_stride,
+                                 k_head_stride, _p(q_weight), _p(k_weight), eps, _p(pos),
+                                 _p(table_cos), _p(table_sin), table_len, rot_dim, pairing,
+                                 _p(q_out), q_out_token_stride, q_out_head_stride, _p(k_out),
+                                 k_out_token_stride, k_out_head_stride, _stream(stream)))
+
+
+def kvb_cache8_append(layout, n_layers, n_seqs, cu_new, max_new, k, v, layer_stride, token_stride,
+                      head_stride, table, lens, k_codes, k_scale, v_codes, v_scale, k_tail, v_tail,
+                      stream=None):
+    _check(_lib.kvb_cache8_append(ctypes.byref(layout), n_layers, n_seqs, _p(cu_new), max_new,
+                                  _p(k), _p(v), layer_stride, token_stride, head_stride,
+                                  _p(table), _p(lens), _p(k_codes), _p(k_scale), _p(v_codes),
+                                  _p(v_scale), _p(k_tail), _p(v_tail), _stream(stream)))
+
+
+def kvb_cache8_read(layout, n_layers, n_seqs, cu_out, max_out, table, lens, k_codes, k_scale,
+                    v_codes, v_scale, k_tail, v_tail, out_dtype, k_out, v_out, layer_stride,
+                    token_stride, head_stride, stream=None):
+    _check(_lib.kvb_cache8_read(ctypes.byref(layout), n_layers, n_seqs, _p(cu_out), max_out,
+                                _p(table), _p(lens), _p(k_codes), _p(k_scale), _p(v_codes),
+                                _p(v_scale), _p(k_tail), _p(v_tail), out_dtype, _p(k_out),
+                                _p(v_out), layer_stride, token_stride, head_stride,
+                                _stream(stream)))
+
+
+def kvb_cache8_attn_workspace_bytes(layout, n_q_heads, n_seqs, n_queries, max_queries, max_len,
+                                    with_weights) -> int:
+    return _lib.kvb_cache8_attn_workspace_bytes(ctypes.byref(layout), n_q_heads, n_seqs, n_queries,
+                                                max_queries, max_len, int(with_weights))
+
+
+def kvb_cache8_attn(layout, n_q_heads, n_seqs, cu_q, n_queries, max_queries, max_len, q, table,
+                    lens, k_codes, k_scale, v_codes, v_scale, k_tail, v_tail, softmax_scale, out,
+                    lse, weights_in, weights_out, workspace, workspace_bytes, stream=None):
+    _check(_lib.kvb_cache8_attn(ctypes.byref(layout), n_q_heads, n_seqs, _p(cu_q), n_queries,
+                                max_queries, max_len, _p(q), _p(table), _p(lens), _p(k_codes),
+                                _p(k_scale), _p(v_codes), _p(v_scale), _p(k_tail), _p(v_tail),
+                                softmax_scale, _p(out), _p(lse), _p(weights_in), _p(weights_out),
+                                _p(workspace), workspace_bytes, _stream(stream)))
+
+
+def kvb_cache8_evict(layout, n_layers, n_seqs, budget, n_first, n_recent, table, lens, weights,
+                     table_out, lens_out, weights_out, stream=None):
+    _check(_lib.kvb_cache8_evict(ctypes.byref(layout), n_layers, n_seqs, budget, n_first, n_recent,
+                                 _p(table), _p(lens), _p(weights), _p(table_out), _p(lens_out),
+                                 _p(weights_out), _stream(stream)))

@@ -1,0 +1,291 @@
+"""Attention over the 8-bit cache against the float64 oracle: block lengths, code
+types and head layouts; lengths from none to long ones around every border; queries
+that see nothing; blocks that are no blocks; values of very different sizes and values
+that are not numbers; split keys; large pools; streams, graphs and repeated calls."""
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+from cache8_check import Cache, attend, check_attention
+from oracle import decode as od
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+def _say(*a):
+    print(*a, file=sys.stderr, flush=True)
+
+
+def _kvb():
+    from paper_2608_21362_amd import kvb
+    return kvb
+
+
+def _q(n, Hq, d, seed, size=1.3):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn((n, Hq, d), generator=g) * size).bfloat16().cuda()
+
+
+def _run(lens, nq, Hq, H, d, B, code, weights=False, seed=0, **kw):
+    c = Cache(lens, H, d, B, code, seed=seed, **kw)
+    q = _q(sum(nq), Hq, d, seed)
+    _say(f"[cache8_attn] lens {lens} queries {nq} heads {Hq}/{H} d {d} B {B} code {code} weights {weights}")
+    kvb = _kvb()
+    win = torch.rand((c.n, H, c.M), device="cuda") if weights else None
+    out, lse, w = attend(kvb, c, c.device(), q, nq, win, weights)
+    torch.cuda.synchronize()
+    check_attention(c, q, nq, out, lse, w, win)
+    return c, q
+
+
+@pytest.mark.parametrize("code", [od.I8, od.E4M3], ids=["i8", "e4m3"])
+@pytest.mark.parametrize("B", [16, 32, 64, 128])
+@pytest.mark.parametrize("d", [64, 128])
+def test_lengths_around_every_border(d, B, code):
+    lens = [1, 2, 15, 16, 17, 63, 64, 65, B - 1, B, B + 1, 127, 128, 129, 3 * B + 5, 257, 0]
+    _run(lens, [1] * len(lens), 8, 2, d, B, code, weights=True)
+
+
+@pytest.mark.parametrize("Hq,H", [(1, 1), (4, 4), (5, 1), (16, 2), (20, 4), (32, 1), (33, 1)])
+def test_head_layouts(Hq, H):
+    _run([200, 77, 500], [1, 1, 1], Hq, H, 128, 32, od.I8, weights=True)
+    _run([200, 77, 500], [2, 0, 7], Hq, H, 64, 16, od.E4M3, weights=True)
+
+
+@pytest.mark.parametrize("nq", [[2], [3, 1], [16, 5], [40], [130, 0, 1], [300]])
+@pytest.mark.parametrize("B,code", [(16, od.E4M3), (64, od.I8), (128, od.I8), (128, od.E4M3)])
+def test_many_queries(nq, B, code):
+    lens = [max(n, 1) + 70 * i + 211 for i, n in enumerate(nq)]
+    _run(lens, nq, 16, 2, 128, B, code, weights=True, seed=3)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_whole_sequence_as_queries(d):
+    """A first turn: every token is a query; the first sees itself alone."""
+    _run([150, 64, 1, 333], [150, 64, 1, 333], 8, 2, d, 64, od.I8, weights=True)
+
+
+def test_queries_that_see_nothing():
+    """More queries than tokens: the first ones see none and get 0 and -infinity."""
+    c, q = _run([3, 0, 40], [7, 2, 41], 8, 2, 64, 16, od.I8, weights=True)
+
+
+@pytest.mark.parametrize("lens", [[4000], [2049, 100, 1], [1027, 1024, 1023, 960]])
+@pytest.mark.parametrize("B,code", [(16, od.I8), (64, od.E4M3), (128, od.I8)])
+def test_split_keys(lens, B, code):
+    """Few tiles and long caches: several workgroups share a tile; every share of the weights arrives."""
+    for nq in ([1] * len(lens), [5] * len(lens)):
+        _run(lens, nq, 16, 2, 128, B, code, weights=True, seed=5)
+        _run(lens, nq, 16, 2, 128, B, code, weights=False, seed=5)
+
+
+@pytest.mark.parametrize("claimed", [1, 100, 640, 5000])
+def test_results_do_not_depend_on_max_len(claimed):
+    c = Cache([1500, 33], 2, 128, 32, od.I8, seed=1, extra=2)
+    q = _q(2, 16, 128, 1)
+    out, lse, w = attend(_kvb(), c, c.device(), q, [1, 1], None, True, max_len=claimed)
+    check_attention(c, q, [1, 1], out, lse, w)
+
+
+def test_value_scales_far_apart():
+    """Scales of V from 2^-30 to 2^30: the small blocks keep their bits where they have the weight."""
+    for code in (od.I8, od.E4M3):
+        _run([700, 515], [1, 9], 8, 2, 128, 32, code, seed=2, spread=30.0)
+    # almost all of the weight on a block a million times smaller than the others
+    c = Cache([256], 1, 128, 64, od.I8, seed=4)
+    k, v = od.bf16(np.random.default_rng(0).standard_normal((256, 128))), od.bf16(np.random.default_rng(1).standard_normal((256, 128)))
+    v[64:128] *= np.float32(2.0 ** -20)
+    q = _q(1, 4, 128, 4)
+    k[70] = od.bf16(8 * q[0].float().mean(0).cpu().numpy())
+    c.put(0, 0, 0, k, v)
+    out, lse, _ = attend(_kvb(), c, c.device(), q, [1])
+    check_attention(c, q, [1], out, lse)
+
+
+def test_small_and_zero_values():
+    """Tiny queries and values, blocks of zeros, whole zero caches."""
+    c = Cache([300, 128], 2, 64, 32, od.I8, seed=6)
+    for (l, b, h), k in list(c.k.items()):
+        rng = np.random.default_rng(h)
+        kk, vv = od.bf16(rng.standard_normal((len(k), 64)) * 1e-30), od.bf16(rng.standard_normal((len(k), 64)) * 1e-33)
+        kk[32:64] = 0
+        vv[:96] = 0
+        if b == 1:
+            vv[:] = 0
+        c.put(l, b, h, kk, vv)
+    q = _q(2, 8, 64, 6, size=1e30)
+    q[:, :, 3] *= 1e-6
+    out, lse, w = attend(_kvb(), c, c.device(), q, [1, 1], None, True)
+    check_attention(c, q, [1, 1], out, lse, w)
+    assert torch.isfinite(out.float()).all() and (out[1] == 0).all()
+
+
+def test_entries_that_are_no_blocks():
+    """Ids outside the pool: their tokens are not seen; a sequence with none left sees nothing."""
+    c = Cache([200, 96, 64], 2, 128, 32, od.E4M3, seed=7)
+    dev = c.device()
+    t = c.table.copy()
+    t[0, 0, :, 1], t[0, 0, 0, 4], t[0, 1, 1, :] = -1, c.N, 2 ** 31 - 1
+    t[0, 2, 0, :2] = -(2 ** 31)
+    dev["table"] = torch.from_numpy(t).cuda()
+    q = _q(3, 8, 128, 7)
+    out, lse, w = attend(_kvb(), c, dev, q, [1, 1, 1], None, True)
+    keep = lambda b, h: np.repeat(  # noqa: E731
+        np.concatenate([(t[0, b, h, :c.lens[b] // 32] >= 0) & (t[0, b, h, :c.lens[b] // 32] < c.N),
+                        np.ones(1, bool)]), 32)[:c.lens[b]]
+    for b in range(3):
+        for h in range(2):
+            m = keep(b, h)
+            for g in range(4):
+                o, e, p = od.attention(q[b, h * 4 + g].float().cpu().numpy()[None], c.k[0, b, h][m], c.v[0, b, h][m], 128 ** -0.5)
+                got = out[b, h * 4 + g].float().cpu().numpy()
+                assert np.all(np.abs(got - o[0]) <= 2.0 ** -8 * np.abs(o[0]) + 2.0 ** -10 * (p @ np.abs(c.v[0, b, h][m]))[0])
+                assert lse[b, h * 4 + g] == -np.inf if not m.any() else abs(lse[b, h * 4 + g].item() - e[0]) < 1e-4
+            gone = ~np.concatenate([(t[0, b, h, :c.lens[b] // 32] >= 0) & (t[0, b, h, :c.lens[b] // 32] < c.N), [True]])
+            w_row = w[b, h].cpu().numpy()
+            assert np.all(w_row[:len(gone)][gone] == 0) and np.all(w_row[c.lens[b] // 32 + 1:] == 0)
+            assert abs(w_row.sum() - (4 if m.any() else 0)) < 1e-3
+
+
+def test_lengths_outside_the_table():
+    """Tokens past the table are not seen; a negative length counts as none."""
+    c = Cache([96, 64, 64], 2, 64, 32, od.I8, seed=8, extra=0)
+    dev = c.device()
+    dev["lens"] = torch.tensor([96 + 70, -5, 64], dtype=torch.int32, device="cuda")
+    q = _q(3, 4, 64, 8)
+    out, lse, w = attend(_kvb(), c, dev, q, [1, 1, 1], None, True, max_len=200)
+    c.lens = np.array([96, 0, 64])
+    for h in range(2):
+        c.k[0, 1, h], c.v[0, 1, h] = c.k[0, 1, h][:0], c.v[0, 1, h][:0]
+    check_attention(c, q, [1, 1, 1], out, lse, w)
+
+
+@pytest.mark.parametrize("code", [od.I8, od.E4M3])
+def test_values_that_are_not_numbers_reach_only_who_sees_them(code):
+    """The last 8 of 200 tokens are queries, and token 196 (in the tail), token 250 of another sequence's
+    last full block and the uninitialised rest of tails and pool are NaN or infinite."""
+    kvb = _kvb()
+    c = Cache([200, 256], 1, 64, 64, code, seed=9)
+    q = _q(8 + 20, 4, 64, 9)
+    k, v = (od.bf16(np.random.default_rng(s).standard_normal((200, 64))) for s in (1, 2))
+    clean_k, clean_v = k.copy(), v.copy()
+    v[196, 3], v[197, 5], k[198, 0] = np.inf, np.nan, np.nan
+    c.put(0, 0, 0, k, v)
+    k2, v2 = (od.bf16(np.random.default_rng(s).standard_normal((256, 64))) for s in (3, 4))
+    v2[250, 1] = np.nan
+    c.put(0, 1, 0, k2, v2)
+    dev = c.device()
+    out, lse, _ = attend(kvb, c, dev, q, [8, 20])
+    o, ls = out.float().cpu().numpy(), lse.cpu().numpy()
+    c.put(0, 0, 0, clean_k, clean_v)
+    for i in range(4):  # queries 192 .. 195 see none of it
+        for h in range(4):
+            r, e, p = od.attention(q[i, h].float().cpu().numpy()[None], c.k[0, 0, 0][:193 + i], c.v[0, 0, 0][:193 + i], 0.125)
+            assert np.all(np.abs(o[i, h] - r[0]) <= 2.0 ** -8 * np.abs(r[0]) + 2.0 ** -10 * (p @ np.abs(c.v[0, 0, 0][:193 + i]))[0])
+    assert np.all(o[4, :, 3] == np.inf) and np.isfinite(np.delete(o[4], 3, 1)).all()
+    assert np.isnan(o[5, :, 5]).all() and np.isfinite(np.delete(o[5], [3, 5], 1)).all()
+    assert np.isnan(o[6:8]).all() and np.isnan(ls[6:8]).all()
+    # every query of the second sequence sees a part of the block with the NaN
+    assert np.isnan(o[8:]).all() and np.isfinite(ls[8:]).all()
+
+
+def test_rows_that_see_none_of_a_block_stay_clean():
+    """Queries before a block whose scale is NaN, in the same tile as queries after it."""
+    c = Cache([192], 1, 128, 64, od.I8, seed=10)
+    k, v = (od.bf16(np.random.default_rng(s).standard_normal((192, 128))) for s in (1, 2))
+    c.put(0, 0, 0, k, v)
+    good = Cache([192], 1, 128, 64, od.I8, seed=10)
+    good.put(0, 0, 0, k, v)
+    k[130, 0], v[140, 0] = np.inf, np.nan
+    c.put(0, 0, 0, k, v)
+    q = _q(80, 4, 128, 10)  # tokens 112 .. 191
+    out, lse, _ = attend(_kvb(), c, c.device(), q, [80])
+    ref, rlse, _ = attend(_kvb(), good, good.device(), q, [80])
+    # both are within 2^-8 of the output and 2^-10 of the largest value of what is exact
+    near = 2.0 ** -7 * ref[:16].float().abs() + 2.0 ** -9 * float(np.abs(v[:128]).max())
+    assert ((out[:16].float() - ref[:16].float()).abs() <= near).all() and torch.equal(lse[:16], rlse[:16])
+    assert torch.isnan(out[16:].float()).all() and torch.isnan(lse[16:]).all()
+
+
+def test_rows_outside_every_sequence_keep_what_they_hold():
+    kvb = _kvb()
+    c = Cache([100, 50], 2, 64, 32, od.I8)
+    q = _q(6, 4, 64, 0)  # 2 + 1 queries, three rows more
+    out, lse, _ = attend(kvb, c, c.device(), q, [2, 1])
+    assert (out[3:] == 7).all() and (lse[3:] == 7).all()
+    check_attention(c, q, [2, 1], out[:3], lse[:3])
+
+
+def test_pool_past_4_gib():
+    """Blocks whose bytes start past 2^32 in both arrays."""
+    kvb = _kvb()
+    N = 600000
+    c = Cache([700], 2, 128, 64, od.E4M3, seed=11)
+    dev = c.device()
+    big = torch.zeros((N, 64, 128), dtype=torch.uint8, device="cuda")
+    bigv = torch.zeros((N, 128, 64), dtype=torch.uint8, device="cuda")
+    move = N - 1 - 7 * torch.arange(c.N, device="cuda")
+    ks, vs = torch.zeros(N, device="cuda"), torch.zeros(N, device="cuda")
+    for name, to in (("k_codes", big), ("v_codes", bigv), ("k_scale", ks), ("v_scale", vs)):
+        to[move] = dev[name]
+        dev[name] = to
+    dev["table"] = move[dev["table"].long()].int()
+    c.N = N
+    q = _q(1, 16, 128, 11)
+    out, lse, w = attend(kvb, c, dev, q, [1], None, True)
+    check_attention(c, q, [1], out, lse, w)
+
+
+def test_weights_in_place_and_from_zero():
+    kvb = _kvb()
+    c = Cache([300], 2, 128, 64, od.I8, extra=4)
+    q, dev, lay = _q(1, 16, 128, 0), c.device(), c.layout(kvb)
+    from cache8_check import cu
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    w = torch.rand((1, 2, c.M), device="cuda")
+    first, out = w.clone(), torch.empty_like(q)
+
+    def call(win, wout):
+        kvb.kvb_cache8_attn(lay, 16, 1, cu([1]), 1, 1, 300, q, dev["table"], dev["lens"], dev["k_codes"],
+                            dev["k_scale"], dev["v_codes"], dev["v_scale"], dev["k_tail"], dev["v_tail"], 128 ** -0.5,
+                            out, None, win, wout, ws, ws.numel())
+
+    call(w, w)
+    share = torch.empty_like(w)
+    call(None, share)
+    assert torch.equal(w, first + share) and abs(share.sum().item() - 16) < 1e-3
+    assert (share[:, :, 300 // 64 + 1:] == 0).all()
+
+
+def test_repeated_calls_and_other_streams_give_the_same_bits():
+    kvb = _kvb()
+    c = Cache([3000, 1500, 7], 2, 128, 32, od.I8, seed=12)
+    dev, q = c.device(), _q(3, 16, 128, 12)
+    ref = attend(kvb, c, dev, q, [1, 1, 1], None, True)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        with torch.cuda.stream(side):
+            got = attend(kvb, c, dev, q, [1, 1, 1], None, True)
+        side.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(ref, got))
+
+
+def test_refusals():
+    kvb = _kvb()
+    c = Cache([64], 2, 64, 32, od.I8)
+    dev, q = c.device(), _q(1, 4, 64, 0)
+    small = torch.empty(16, dtype=torch.uint8, device="cuda")
+    with pytest.raises(kvb.KvbError) as e:
+        kvb.kvb_cache8_attn(c.layout(kvb), 4, 1, q, 1, 1, 100000, q, dev["table"], dev["lens"], dev["k_codes"],
+                            dev["k_scale"], dev["v_codes"], dev["v_scale"], dev["k_tail"], dev["v_tail"], 0.1, q, None,
+                            None, None, small, 16)
+    assert e.value.status == kvb.KVB_EINVAL and "workspace" in e.value.message
