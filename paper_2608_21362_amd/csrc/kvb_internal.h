@@ -158,8 +158,10 @@ struct Attn8Plan {
   int n_tiles;         // query tiles per (sequence, kv head)
   int n_splits;        // workgroups that share a tile's keys
   int span;            // 64-key steps of each but the last
-  int64_t rows;        // query rows of a (sequence, kv head), at most
-  int64_t n_parts;     // parts of up to 64 tokens of a block with a weight of their own
+  int wave_span;       // steps of a wave of it
+  int group;           // query heads of a kv head
+  int rows;            // query rows of a (sequence, kv head), at most
+  int n_parts;         // parts of up to 64 tokens of a block with a weight of their own
   size_t ml_offset;    // (max, sum) of each (sequence, kv head, split, row)
   size_t parts_offset; // log2 weight of each (sequence, kv head, part, row)
   size_t workspace;    // total bytes
