@@ -309,49 +309,149 @@ __device__ __forceinline__ uint32_t order_key(float x) {
   return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
-// One workgroup per table row.  The k-th largest key of the middle blocks is found
-// digit by digit (8 bits) from counts in LDS; the row is then written in order with
-// the ranks of kept and dropped entries from ballots.  Counts decide, so the result
-// does not depend on the order of the atomics.
-__global__ void __launch_bounds__(256) evict_kernel(Evict a) {
-  __shared__ int32_t bins[256], wave_kept[4], wave_ties[4];
-  __shared__ uint32_t s_prefix;
-  __shared__ int32_t s_left;
-  const int64_t row = blockIdx.x;
-  const int b = (int)(row / a.n_kv_heads % a.n_seqs);
-  const int M = a.max_blocks, tid = threadIdx.x;
+// What a table row keeps: nb full blocks of M entries, `drop` of them leave; the k best of the
+// blocks [lo, hi) stay, and all others below nb.
+struct Row {
+  int nb, drop, lo, hi, k;
+};
+__device__ __forceinline__ Row row_of(const Evict& a, int b) {
+  Row r;
+  const int len = max(a.lens[b], 0);
+  r.nb = min(len / a.block_len, a.max_blocks);
+  r.drop = r.nb > a.budget ? r.nb - a.budget : 0;
+  r.lo = a.n_first, r.hi = r.nb - a.n_recent;
+  r.k = a.budget - a.n_first - a.n_recent;
+  return r;
+}
+
+// A wave a row of up to 64 * N entries, all in registers (lane i: entries i, i + 64, ..), so the row
+// is read once and nothing waits for another wave.  The k-th largest key is found bit by bit: a
+// key set's count is a ballot's population count, and the search ends when it is k.
+// (18432 rows of 902 entries, 266 MB: 329 us with a workgroup a row and counts of digits in LDS.)
+template <int N>
+__global__ void __launch_bounds__(256) evict_wave_kernel(Evict a, int64_t rows) {
+  const int lane = threadIdx.x & 63;
+  const int64_t row = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
+  if (row >= rows) return;
+  const int b = (int)((uint32_t)row / (uint32_t)a.n_kv_heads % (uint32_t)a.n_seqs);
+  const int M = a.max_blocks;
   const int32_t* table = a.table + row * M;
   const float* weights = a.weights + row * M;
   int32_t* table_out = a.table_out + row * M;
   float* weights_out = a.weights_out + row * M;
-  const int32_t len = max(a.lens[b], 0);
-  const int nb = min(len / a.block_len, M);
-  const int drop = nb > a.budget ? nb - a.budget : 0;
-  if (row / a.n_kv_heads < a.n_seqs && row % a.n_kv_heads == 0 && tid == 0)
-    a.lens_out[b] = a.lens[b] - drop * a.block_len;
-  if (drop == 0) {
-    for (int i = tid; i < M; i += 256) table_out[i] = table[i], weights_out[i] = weights[i];
+  int32_t t[N];
+  float w[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const int i = min(j * 64 + lane, M - 1);
+    t[j] = table[i];
+    w[j] = weights[i];
+  }
+  const Row r = row_of(a, b);
+  if (row < (int64_t)a.n_seqs * a.n_kv_heads && row % a.n_kv_heads == 0 && lane == 0)
+    a.lens_out[b] = a.lens[b] - r.drop * a.block_len;
+  // the k-th largest key of the competing blocks; the others have key 0, and every candidate is larger
+  uint32_t key[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const int i = j * 64 + lane;
+    key[j] = i >= r.lo && i < r.hi ? order_key(w[j]) : 0u;
+  }
+  uint32_t kth = 0;
+  int left = 0x7FFFFFFF;  // of the keys equal to kth, this many are kept
+  if (r.drop > 0 && r.k > 0) {
+    int found = 0;
+    for (uint32_t bit = 0x80000000u; bit != 0 && found != r.k; bit >>= 1) {
+      const uint32_t candidate = kth | bit;
+      int n = 0;
+#pragma unroll
+      for (int j = 0; j < N; ++j) n += __popcll(__ballot(key[j] >= candidate));
+      if (n >= r.k) kth = candidate, found = n;
+    }
+    if (found != r.k) {  // equal keys on both sides of the cut: the lower indices stay
+      int n = 0;
+#pragma unroll
+      for (int j = 0; j < N; ++j) n += __popcll(__ballot(key[j] > kth));
+      left = r.k - n;
+    }
+  }
+  const uint64_t below = (1ull << lane) - 1;
+  int kept = 0, ties = 0;  // before this register's entries
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const int i = j * 64 + lane;
+    const bool middle = i >= r.lo && i < r.hi;
+    int to;
+    float x = w[j];
+    if (r.drop == 0) {
+      to = i;
+    } else {
+      const bool tie = middle && r.k > 0 && key[j] == kth;
+      const uint64_t tm = __ballot(tie);
+      const bool keep = i < r.nb && (!middle || (r.k > 0 && (key[j] > kth || (tie && ties + __popcll(tm & below) < left))));
+      const uint64_t km = __ballot(keep);
+      const int before = kept + __popcll(km & below);
+      to = i >= r.nb ? i - r.drop : keep ? before : M - r.drop + (i - before);
+      if (!keep && i < r.nb) x = 0.f;
+      kept += __popcll(km);
+      ties += __popcll(tm);
+    }
+    if (i < M) table_out[to] = t[j], weights_out[to] = x;
+  }
+}
+
+// One workgroup per table row of any length.  The k-th largest key of the middle blocks is found
+// digit by digit (8 bits) from counts in LDS; the row is then written in order with the ranks of
+// kept and dropped entries from ballots.  Counts decide, so the result does not depend on the
+// order of the atomics.
+constexpr int kEvictWaves = 16;
+__global__ void __launch_bounds__(64 * kEvictWaves) evict_kernel(Evict a) {
+  constexpr int T = 64 * kEvictWaves;
+  __shared__ int32_t bins[256], wave_kept[kEvictWaves], wave_ties[kEvictWaves];
+  __shared__ uint32_t s_prefix;
+  __shared__ int32_t s_left;
+  const int64_t row = blockIdx.x;
+  const int b = (int)((uint32_t)row / (uint32_t)a.n_kv_heads % (uint32_t)a.n_seqs);
+  const int M = a.max_blocks, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int32_t* table = a.table + row * M;
+  const float* weights = a.weights + row * M;
+  int32_t* table_out = a.table_out + row * M;
+  float* weights_out = a.weights_out + row * M;
+  const Row r = row_of(a, b);
+  if (row < (int64_t)a.n_seqs * a.n_kv_heads && row % a.n_kv_heads == 0 && tid == 0)
+    a.lens_out[b] = a.lens[b] - r.drop * a.block_len;
+  if (r.drop == 0) {
+    for (int i = tid; i < M; i += T) table_out[i] = table[i], weights_out[i] = weights[i];
     return;
   }
-  const int lo = a.n_first, hi = nb - a.n_recent;  // the blocks that compete
-  const int k = a.budget - a.n_first - a.n_recent;
   uint32_t prefix = 0;
-  int left = k;  // of the keys that start with prefix, the `left` largest are kept
-  if (k > 0) {
+  int left = r.k;  // of the keys that start with prefix, the `left` largest are kept
+  if (r.k > 0) {
     for (int shift = 24; shift >= 0; shift -= 8) {
-      bins[tid] = 0;
+      if (tid < 256) bins[tid] = 0;
       __syncthreads();
-      for (int i = lo + tid; i < hi; i += 256) {
+      for (int i = r.lo + tid; i < r.hi; i += T) {
         const uint32_t key = order_key(weights[i]);
         if (shift == 24 || key >> (shift + 8) == prefix >> (shift + 8))
           atomicAdd(&bins[key >> shift & 255], 1);
       }
       __syncthreads();
-      if (tid == 0) {
-        int above = 0, d = 255;
-        while (d > 0 && above + bins[d] < left) above += bins[d--];
-        s_prefix = prefix | (uint32_t)d << shift;
-        s_left = left - above;
+      if (wave == 0) {  // a lane four bins, the largest digits first
+        int n[4], sum = 0;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) sum += n[q] = bins[255 - 4 * lane - q];
+        int upto = sum;  // keys in the bins of lanes 0 .. lane
+        for (int x = 1; x < 64; x <<= 1) {
+          const int y = __shfl_up(upto, x, 64);
+          if (lane >= x) upto += y;
+        }
+        int above = upto - sum;
+        if (above < left && upto >= left) {  // one lane: the digit is among its four
+          int q = 0;
+          while (above + n[q] < left) above += n[q++];
+          s_prefix = prefix | (uint32_t)(255 - 4 * lane - q) << shift;
+          s_left = left - above;
+        }
       }
       __syncthreads();
       prefix = s_prefix;
@@ -360,39 +460,39 @@ __global__ void __launch_bounds__(256) evict_kernel(Evict a) {
   }
   // kept: forced, above the k-th key, or among the first `left` equal to it
   int kept_before = 0, ties_before = 0;
-  for (int base = 0; base < nb; base += 256) {
+  for (int base = 0; base < r.nb; base += T) {
     const int i = base + tid;
-    const bool in = i < nb, middle = in && i >= lo && i < hi;
+    const bool in = i < r.nb, middle = in && i >= r.lo && i < r.hi;
     const float w = in ? weights[i] : 0.f;
     const uint32_t key = order_key(w);
-    const bool tie = middle && k > 0 && key == prefix;
-    const uint64_t tm = __ballot(tie), below = (1ull << (tid & 63)) - 1;
-    if ((tid & 63) == 0) wave_ties[tid >> 6] = __popcll(tm);
+    const bool tie = middle && r.k > 0 && key == prefix;
+    const uint64_t tm = __ballot(tie), below = (1ull << lane) - 1;
+    if (lane == 0) wave_ties[wave] = __popcll(tm);
     __syncthreads();
     int ties = ties_before + __popcll(tm & below);
-    for (int q = 0; q < 4; ++q) {
-      if (q < tid >> 6) ties += wave_ties[q];
+    for (int q = 0; q < kEvictWaves; ++q) {
+      if (q < wave) ties += wave_ties[q];
       ties_before += wave_ties[q];
     }
-    const bool keep = in && (!middle || (k > 0 && (key > prefix || (tie && ties < left))));
+    const bool keep = in && (!middle || (r.k > 0 && (key > prefix || (tie && ties < left))));
     const uint64_t km = __ballot(keep);
-    if ((tid & 63) == 0) wave_kept[tid >> 6] = __popcll(km);
+    if (lane == 0) wave_kept[wave] = __popcll(km);
     __syncthreads();
     int kept = kept_before + __popcll(km & below);
-    for (int q = 0; q < 4; ++q) {
-      if (q < tid >> 6) kept += wave_kept[q];
+    for (int q = 0; q < kEvictWaves; ++q) {
+      if (q < wave) kept += wave_kept[q];
       kept_before += wave_kept[q];
     }
     if (in) {
-      const int to = keep ? kept : M - drop + (i - kept);
+      const int to = keep ? kept : M - r.drop + (i - kept);
       table_out[to] = table[i];
       weights_out[to] = keep ? w : 0.f;
     }
     __syncthreads();
   }
-  for (int i = nb + tid; i < M; i += 256) {
-    table_out[i - drop] = table[i];
-    weights_out[i - drop] = weights[i];
+  for (int i = r.nb + tid; i < M; i += T) {
+    table_out[i - r.drop] = table[i];
+    weights_out[i - r.drop] = weights[i];
   }
 }
 
@@ -465,7 +565,14 @@ hipError_t launch_cache8_read(const Cache8& c, int head_dim, int block_len, int 
 
 hipError_t launch_cache8_evict(const Evict& a, int n_layers, hipStream_t s) {
   const int64_t rows = (int64_t)n_layers * a.n_seqs * a.n_kv_heads;
-  hipLaunchKernelGGL(evict_kernel, dim3((unsigned)rows), dim3(256), 0, s, a);
+  const dim3 grid((unsigned)((rows + 3) / 4));
+#define KVB_EVICT(N) hipLaunchKernelGGL(evict_wave_kernel<N>, grid, dim3(256), 0, s, a, rows)
+  if (a.max_blocks <= 256) KVB_EVICT(4);
+  else if (a.max_blocks <= 512) KVB_EVICT(8);
+  else if (a.max_blocks <= 1024) KVB_EVICT(16);
+  else if (a.max_blocks <= 2048) KVB_EVICT(32);
+  else hipLaunchKernelGGL(evict_kernel, dim3((unsigned)rows), dim3(64 * kEvictWaves), 0, s, a);
+#undef KVB_EVICT
   return hipGetLastError();
 }
 
