@@ -705,12 +705,14 @@ static kvb_status check_cache8_arrays(const void* const* ptrs, int n) {
   return KVB_OK;
 }
 
-static kvb::Cache8 cache8_of(const kvb_cache8_layout* p, int32_t n_seqs, const int32_t* table,
+static kvb::Cache8 cache8_of(const kvb_cache8_layout* p, int32_t n_layers, int32_t n_seqs,
+                             const int32_t* table,
                              const int32_t* lens, const uint8_t* k_codes, const float* k_scale,
                              const uint8_t* v_codes, const float* v_scale, const uint16_t* k_tail,
                              const uint16_t* v_tail) {
   kvb::Cache8 c{};
   c.n_blocks = p->n_blocks, c.n_kv_heads = p->n_kv_heads, c.n_seqs = n_seqs;
+  c.n_rows = n_layers * n_seqs * p->n_kv_heads;
   c.max_blocks = p->max_blocks;
   c.table = table, c.lens = lens;
   c.k_codes = const_cast<uint8_t*>(k_codes), c.v_codes = const_cast<uint8_t*>(v_codes);
@@ -734,9 +736,9 @@ kvb_status kvb_cache8_append(const kvb_cache8_layout* layout, int32_t n_layers, 
   const void* ptrs[] = {k, v, k_codes, k_scale, v_codes, v_scale, k_tail, v_tail};
   if (kvb_status s = check_cache8_arrays(ptrs, 8)) return s;
   return hip_status(
-      kvb::launch_cache8_append(cache8_of(layout, n_seqs, table, lens, k_codes, k_scale, v_codes,
+      kvb::launch_cache8_append(cache8_of(layout, n_layers, n_seqs, table, lens, k_codes, k_scale, v_codes,
                                           v_scale, k_tail, v_tail),
-                                layout->head_dim, layout->block_len, layout->code, n_layers, cu_new,
+                                layout->head_dim, layout->block_len, layout->code, cu_new,
                                 max_new, k, v, layer_stride, token_stride, head_stride,
                                 (hipStream_t)stream),
       "kvb_cache8_append");
@@ -759,9 +761,9 @@ kvb_status kvb_cache8_read(const kvb_cache8_layout* layout, int32_t n_layers, in
   const void* ptrs[] = {k_out, v_out, k_codes, k_scale, v_codes, v_scale, k_tail, v_tail};
   if (kvb_status s = check_cache8_arrays(ptrs, 8)) return s;
   return hip_status(
-      kvb::launch_cache8_read(cache8_of(layout, n_seqs, table, lens, k_codes, k_scale, v_codes,
+      kvb::launch_cache8_read(cache8_of(layout, n_layers, n_seqs, table, lens, k_codes, k_scale, v_codes,
                                         v_scale, k_tail, v_tail),
-                              layout->head_dim, layout->block_len, layout->code, n_layers, cu_out,
+                              layout->head_dim, layout->block_len, layout->code, cu_out,
                               max_out, out_dtype, k_out, v_out, layer_stride, token_stride,
                               head_stride, (hipStream_t)stream),
       "kvb_cache8_read");
@@ -814,7 +816,7 @@ kvb_status kvb_cache8_attn(const kvb_cache8_layout* layout, int32_t n_q_heads, i
   if (plan.workspace)
     REQUIRE(workspace != nullptr && aligned16(workspace), "workspace NULL or misaligned");
   kvb::Attn8 a{};
-  a.c = cache8_of(layout, n_seqs, table, lens, k_codes, k_scale, v_codes, v_scale, k_tail, v_tail);
+  a.c = cache8_of(layout, 1, n_seqs, table, lens, k_codes, k_scale, v_codes, v_scale, k_tail, v_tail);
   a.n_q_heads = n_q_heads, a.n_queries = n_queries;
   a.cu_q = cu_q, a.q = q, a.out = out, a.lse = lse, a.softmax_scale = softmax_scale;
   a.weights_in = weights_in, a.weights_out = weights_out;

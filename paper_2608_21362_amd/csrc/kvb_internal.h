@@ -128,17 +128,18 @@ hipError_t launch_qk_norm_rope(const QkNormRope& a, kvb_dtype dtype, hipStream_t
 
 struct Cache8 {
   int32_t n_blocks, n_kv_heads, n_seqs, max_blocks;
+  int32_t n_rows;  // table rows: layers x sequences x kv heads
   const int32_t *table, *lens;
   uint8_t *k_codes, *v_codes;
   float *k_scale, *v_scale;
   uint16_t *k_tail, *v_tail;
 };
-hipError_t launch_cache8_append(const Cache8& c, int head_dim, int block_len, int code, int n_layers,
+hipError_t launch_cache8_append(const Cache8& c, int head_dim, int block_len, int code,
                                 const int32_t* cu_new, int max_new, const uint16_t* k,
                                 const uint16_t* v, int64_t layer_stride, int64_t token_stride,
                                 int64_t head_stride, hipStream_t s);
 // only reads the cache
-hipError_t launch_cache8_read(const Cache8& c, int head_dim, int block_len, int code, int n_layers,
+hipError_t launch_cache8_read(const Cache8& c, int head_dim, int block_len, int code,
                               const int32_t* cu_out, int max_out, kvb_dtype dtype, void* k, void* v,
                               int64_t layer_stride, int64_t token_stride, int64_t head_stride,
                               hipStream_t s);
