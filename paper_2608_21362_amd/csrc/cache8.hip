@@ -151,20 +151,57 @@ constexpr int kRowsY = 32768;  // grid rows (K and V of table rows) in y, the ot
 
 // ---- append ---------------------------------------------------------------
 
-// The tail rows [from, to) of block j of one sequence and head, from the new rows.
+// 16-bit numbers of 2 words of 4 rows, turned: word w of the rows -> words of the 4 rows' low halves
+// (lo) and high halves (hi)
+__device__ __forceinline__ void turn4x2(const uint32_t* in, uint2& lo, uint2& hi) {
+  lo = make_uint2(__builtin_amdgcn_perm(in[1], in[0], 0x05040100u), __builtin_amdgcn_perm(in[3], in[2], 0x05040100u));
+  hi = make_uint2(__builtin_amdgcn_perm(in[1], in[0], 0x07060302u), __builtin_amdgcn_perm(in[3], in[2], 0x07060302u));
+}
+__device__ __forceinline__ uint32_t word_of(const uint4& x, int w) {
+  return w == 0 ? x.x : w == 1 ? x.y : w == 2 ? x.z : x.w;
+}
+
+// The tail rows [from, to) of a block from the new rows (`rows`: row `from`).  V: a thread takes 4
+// tokens x 8 channels, neighbouring lanes neighbouring tokens, so that a wave's stores are runs of
+// a channel (one token a thread stored single numbers 2 B apart: 40 us of the 206 above).
 template <int D, int B>
 __device__ __forceinline__ void write_tail(int is_v, uint16_t* tail, const uint16_t* rows,
                                            int64_t token_stride, int from, int to) {
   constexpr int PPR = D / 8;  // 16-byte pieces of a row
-  for (int i = threadIdx.x; i < (to - from) * PPR; i += blockDim.x) {
-    const int u = i / PPR, c = i % PPR * 8;
-    const uint4 x = *reinterpret_cast<const uint4*>(rows + (int64_t)u * token_stride + c);
-    if (!is_v) {
-      *reinterpret_cast<uint4*>(tail + (from + u) * D + c) = x;
-    } else {
-      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  if (!is_v) {
+    for (int i = threadIdx.x; i < (to - from) * PPR; i += blockDim.x) {
+      const int u = i / PPR, c = i % PPR * 8;
+      *reinterpret_cast<uint4*>(tail + (from + u) * D + c) =
+          *reinterpret_cast<const uint4*>(rows + (int64_t)u * token_stride + c);
+    }
+    return;
+  }
+  const int q0 = from / 4, quads = (to + 3) / 4 - q0;
+  for (int i = threadIdx.x; i < quads * PPR; i += blockDim.x) {
+    const int u = (q0 + i % quads) * 4, c = i / quads * 8;
+    uint4 x[4];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) tail[(c + e) * B + from + u] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
+    for (int e = 0; e < 4; ++e) {
+      const int t = min(max(u + e, from), to - 1);
+      x[e] = *reinterpret_cast<const uint4*>(rows + (int64_t)(t - from) * token_stride + c);
+    }
+    const bool whole = u >= from && u + 4 <= to;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const uint32_t in[4] = {word_of(x[0], w), word_of(x[1], w), word_of(x[2], w), word_of(x[3], w)};
+      uint2 y[2];
+      turn4x2(in, y[0], y[1]);
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        uint16_t* at = tail + (c + 2 * w + z) * B + u;
+        if (whole) {
+          *reinterpret_cast<uint2*>(at) = y[z];
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (u + e >= from && u + e < to) at[e] = (uint16_t)((e < 2 ? y[z].x : y[z].y) >> (16 * (e & 1)));
+        }
+      }
     }
   }
 }
@@ -178,7 +215,7 @@ append_kernel(Cache8 c, const int32_t* __restrict__ cu, const uint16_t* __restri
   constexpr int WAVES = Q::THREADS / 64;
   __shared__ uint32_t wave_max[WAVES];
   __shared__ __align__(16) uint8_t turned[D * Q::LDT];
-  const int row = blockIdx.y + blockIdx.z * kRowsY >> 1, is_v = blockIdx.y & 1;  // row: (layer, sequence, kv head)
+  const int row = (int)(blockIdx.y + blockIdx.z * kRowsY) >> 1, is_v = blockIdx.y & 1;  // row: (layer, sequence, kv head)
   if (row >= c.n_rows) return;
   const int b = row / c.n_kv_heads % c.n_seqs;
   const Span sp = span_of(cu, c.lens, b, B);
@@ -304,13 +341,21 @@ __device__ __forceinline__ void store8(uint16_t* p, const float* x) {
                                             pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
 }
 
+// 8 bfloat16 as they are
+__device__ __forceinline__ void store8(uint16_t* p, const uint4& x) { *reinterpret_cast<uint4*>(p) = x; }
+__device__ __forceinline__ void store8(float* p, const uint4& x) {
+  const float f[8] = {bf16_lo(x.x), bf16_hi(x.x), bf16_lo(x.y), bf16_hi(x.y),
+                      bf16_lo(x.z), bf16_hi(x.z), bf16_lo(x.w), bf16_hi(x.w)};
+  store8(p, f);
+}
+
 template <int D, int B, int CODE, typename T>
 __global__ void __launch_bounds__((Quads<D, B>::THREADS))
 read_kernel(Cache8 c, const int32_t* __restrict__ cu, T* __restrict__ k, T* __restrict__ v,
             int64_t layer_stride, int64_t token_stride, int64_t head_stride) {
   typedef Quads<D, B> Q;
   __shared__ __align__(16) uint8_t turned[D * Q::LDT];
-  const int row = blockIdx.y + blockIdx.z * kRowsY >> 1, is_v = blockIdx.y & 1;
+  const int row = (int)(blockIdx.y + blockIdx.z * kRowsY) >> 1, is_v = blockIdx.y & 1;
   if (row >= c.n_rows) return;
   const int b = row / c.n_kv_heads % c.n_seqs;
   const Span sp = span_of(cu, c.lens, b, B);
@@ -371,13 +416,29 @@ read_kernel(Cache8 c, const int32_t* __restrict__ cu, T* __restrict__ k, T* __re
         }
       }
     } else if (j <= c.max_blocks) {
-      for (int p = threadIdx.x + from * Q::PPR; p < to * Q::PPR; p += Q::THREADS) {
-        const int u = p / Q::PPR, cc = p % Q::PPR * 8;
-        float x[8];
+      if (!is_v) {
+        for (int p = threadIdx.x + from * Q::PPR; p < to * Q::PPR; p += Q::THREADS) {
+          const int u = p / Q::PPR, cc = p % Q::PPR * 8;
+          store8(out + (int64_t)u * token_stride + cc, *reinterpret_cast<const uint4*>(tail + u * D + cc));
+        }
+      } else {  // as write_tail, the other way
+        const int q0 = from / 4, quads = (to + 3) / 4 - q0;
+        for (int p = threadIdx.x; p < quads * Q::PPR; p += Q::THREADS) {
+          const int u = (q0 + p % quads) * 4, cc = p / quads * 8;
+          uint2 y[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          x[e] = bf16_lo(is_v ? tail[(cc + e) * B + u] : tail[u * D + cc + e]);
-        store8(out + (int64_t)u * token_stride + cc, x);
+          for (int e = 0; e < 8; ++e) y[e] = *reinterpret_cast<const uint2*>(tail + (cc + e) * B + u);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            uint32_t w[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              w[q] = __builtin_amdgcn_perm(e < 2 ? y[2 * q + 1].x : y[2 * q + 1].y, e < 2 ? y[2 * q].x : y[2 * q].y,
+                                           e & 1 ? 0x07060302u : 0x05040100u);
+            if (u + e >= from && u + e < to)
+              store8(out + (int64_t)(u + e) * token_stride + cc, make_uint4(w[0], w[1], w[2], w[3]));
+          }
+        }
       }
     }
   }
