@@ -115,7 +115,7 @@ hipError_t launch_sparse_attn_layer(const AttnPlan& layer_plan, int layer, int n
 struct QkNormRope {
   int64_t n_tokens;
   int32_t n_q_heads, n_kv_heads, head_dim, rot_dim, pairing, table_len;
-  int32_t chunks;  // waves per token (set by the launcher)
+  int32_t q_chunks, k_chunks;  // waves of a token's queries and keys (set by the launcher)
   float eps;
   const void *q, *k;
   const float *q_weight, *k_weight, *table_cos, *table_sin;

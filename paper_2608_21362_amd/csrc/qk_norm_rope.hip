@@ -16,6 +16,8 @@
 namespace kvb {
 namespace {
 
+constexpr int kGroups = 4;  // head groups of a wave where there are many waves
+
 // x from the lane chosen by DPP control CTRL
 template <int CTRL>
 __device__ __forceinline__ float dpp(float x) {
@@ -33,14 +35,27 @@ __device__ __forceinline__ float head_sum(float x) {
   return x;
 }
 
-// 4 consecutive values as floats
+// 4 consecutive values, as they are held, and as floats
+template <typename T>
+struct Four;
+template <>
+struct Four<float> {
+  float4 v;
+  __device__ __forceinline__ void load(const float* p) { v = *reinterpret_cast<const float4*>(p); }
+  __device__ __forceinline__ void get(float* x) const { x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w; }
+};
+template <>
+struct Four<uint16_t> {
+  uint2 v;
+  __device__ __forceinline__ void load(const uint16_t* p) { v = *reinterpret_cast<const uint2*>(p); }
+  __device__ __forceinline__ void get(float* x) const {
+    x[0] = bf16_lo(v.x), x[1] = bf16_hi(v.x), x[2] = bf16_lo(v.y), x[3] = bf16_hi(v.y);
+  }
+};
 __device__ __forceinline__ void load4(const float* p, float* x) {
-  const float4 v = *reinterpret_cast<const float4*>(p);
-  x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
-}
-__device__ __forceinline__ void load4(const uint16_t* p, float* x) {
-  const uint2 v = *reinterpret_cast<const uint2*>(p);
-  x[0] = bf16_lo(v.x), x[1] = bf16_hi(v.x), x[2] = bf16_lo(v.y), x[3] = bf16_hi(v.y);
+  Four<float> f;
+  f.load(p);
+  f.get(x);
 }
 __device__ __forceinline__ void store4(float* p, const float* x) {
   *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
@@ -53,30 +68,35 @@ template <typename T, int LPH, int U>
 __global__ void __launch_bounds__(256) qk_norm_rope_kernel(QkNormRope a) {
   constexpr int HPW = 64 / LPH;  // heads of a group
   const int lane = threadIdx.x & 63, u = lane % LPH;
-  const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int64_t t = wave / a.chunks;
-  const int g0 = (int)(wave % a.chunks) * U * HPW + lane / LPH;  // first head of this lane
+  // what the wave takes, on the scalar unit: a token, and groups of either queries or keys
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+  const uint32_t chunks = a.q_chunks + a.k_chunks;
+  const int64_t t = wave / chunks;
   if (t >= a.n_tokens) return;
-  const int heads = a.n_q_heads + a.n_kv_heads;
+  const int chunk = (int)(wave - (uint32_t)t * chunks);
+  const bool is_q = chunk < a.q_chunks;
+  const int h0 = (is_q ? chunk : chunk - a.q_chunks) * U * HPW, heads = is_q ? a.n_q_heads : a.n_kv_heads;
+  const T* from = is_q ? (const T*)a.q + t * a.q_token_stride : (const T*)a.k + t * a.k_token_stride;
+  T* to = is_q ? (T*)a.q_out + t * a.q_out_token_stride : (T*)a.k_out + t * a.k_out_token_stride;
+  const int64_t from_head = is_q ? a.q_head_stride : a.k_head_stride;
+  const int64_t to_head = is_q ? a.q_out_head_stride : a.k_out_head_stride;
+  const float* weight = is_q ? a.q_weight : a.k_weight;
   const bool in = u * 8 < a.head_dim, turns = u * 8 < a.rot_dim;
   // where the unit's two runs of 4 channels start
   const bool split = turns && a.pairing == KVB_PAIR_HALF;
   const int c0 = split ? 4 * u : 8 * u, c1 = split ? a.rot_dim / 2 + 4 * u : 8 * u + 4;
-  float x[U][8];
+  Four<T> x[U][2];
 #pragma unroll
   for (int k = 0; k < U; ++k) {
-    const int h = g0 + k * HPW;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[k][e] = 0.f;
+    const int h = h0 + k * HPW + lane / LPH;
+    x[k][0] = x[k][1] = Four<T>{};
     if (in && h < heads) {
-      const T* p = h < a.n_q_heads
-                       ? (const T*)a.q + t * a.q_token_stride + h * a.q_head_stride
-                       : (const T*)a.k + t * a.k_token_stride + (h - a.n_q_heads) * a.k_head_stride;
-      load4(p + c0, x[k]);
-      load4(p + c1, x[k] + 4);
+      x[k][0].load(from + h * from_head + c0);
+      x[k][1].load(from + h * from_head + c1);
     }
   }
-  float c[4] = {1.f, 1.f, 1.f, 1.f}, s[4] = {0.f, 0.f, 0.f, 0.f};
+  float w[8], c[4] = {1.f, 1.f, 1.f, 1.f}, s[4] = {0.f, 0.f, 0.f, 0.f};
+  if (weight != nullptr && in) load4(weight + c0, w), load4(weight + c1, w + 4);
   bool bad = false;
   if (a.rot_dim > 0) {
     const int pos = a.pos[t];
@@ -86,25 +106,22 @@ __global__ void __launch_bounds__(256) qk_norm_rope_kernel(QkNormRope a) {
       load4(a.table_sin + (int64_t)pos * (a.rot_dim / 2) + 4 * u, s);
     }
   }
-  float wq[8], wk[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) wq[e] = wk[e] = 1.f;
-  if (in && a.q_weight) load4(a.q_weight + c0, wq), load4(a.q_weight + c1, wq + 4);
-  if (in && a.k_weight) load4(a.k_weight + c0, wk), load4(a.k_weight + c1, wk + 4);
 #pragma unroll
   for (int k = 0; k < U; ++k) {
-    const int h = g0 + k * HPW;
-    const bool is_q = h < a.n_q_heads;
-    float sum = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(x[k][e], x[k][e], sum);
-    sum = head_sum<LPH>(sum);
-    if (!in || h >= heads) continue;
-    const bool norm = is_q ? a.q_weight != nullptr : a.k_weight != nullptr;
-    const float r = norm ? 1.f / sqrtf(sum / (float)a.head_dim + a.eps) : 1.f;
+    const int h = h0 + k * HPW + lane / LPH;
     float y[8], z[8];
+    x[k][0].get(y);
+    x[k][1].get(y + 4);
+    if (weight != nullptr) {
+      float sum = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = norm ? x[k][e] * r * (is_q ? wq[e] : wk[e]) : x[k][e];
+      for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(y[e], y[e], sum);
+      sum = head_sum<LPH>(sum);
+      const float r = 1.f / sqrtf(sum / (float)a.head_dim + a.eps);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = y[e] * r * w[e];
+    }
+    if (!in || h >= heads) continue;
     if (a.pairing == KVB_PAIR_HALF) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -120,21 +137,23 @@ __global__ void __launch_bounds__(256) qk_norm_rope_kernel(QkNormRope a) {
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) z[e] = bad ? __builtin_nanf("") : turns ? z[e] : y[e];
-    T* p = is_q ? (T*)a.q_out + t * a.q_out_token_stride + h * a.q_out_head_stride
-                : (T*)a.k_out + t * a.k_out_token_stride + (h - a.n_q_heads) * a.k_out_head_stride;
-    store4(p + c0, z);
-    store4(p + c1, z + 4);
+    store4(to + h * to_head + c0, z);
+    store4(to + h * to_head + c1, z + 4);
   }
 }
 
 template <typename T, int LPH>
 void launch(QkNormRope a, hipStream_t s) {
-  constexpr int HPW = 64 / LPH, U = 4;
-  const int groups = (a.n_q_heads + a.n_kv_heads + HPW - 1) / HPW;
-  a.chunks = (groups + U - 1) / U;
-  const int64_t waves = a.n_tokens * a.chunks;
-  hipLaunchKernelGGL((qk_norm_rope_kernel<T, LPH, U>), dim3((unsigned)((waves + 3) / 4)), dim3(256),
-                     0, s, a);
+  constexpr int HPW = 64 / LPH;
+  const int gq = (a.n_q_heads + HPW - 1) / HPW, gk = (a.n_kv_heads + HPW - 1) / HPW;
+  // Few waves: one group each, so that the loads of a call spread over the card.
+  const int u = a.n_tokens * (gq + gk) <= 4096 ? 1 : kGroups;
+  a.q_chunks = (gq + u - 1) / u;
+  a.k_chunks = (gk + u - 1) / u;
+  const int64_t waves = a.n_tokens * (a.q_chunks + a.k_chunks);
+  const dim3 grid((unsigned)((waves + 3) / 4));
+  if (u == 1) hipLaunchKernelGGL((qk_norm_rope_kernel<T, LPH, 1>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((qk_norm_rope_kernel<T, LPH, kGroups>), grid, dim3(256), 0, s, a);
 }
 
 }  // namespace
