@@ -540,7 +540,7 @@ kvb_status kvb_qk_norm_rope(int64_t n_tokens, int32_t n_q_heads, int32_t n_kv_he
  *   k_scale/v_scale f32  [n_blocks]
  *   k_tail          bf16 [L][n_seqs][Hkv][B][d]
  *   v_tail          bf16 [L][n_seqs][Hkv][d][B]         (channel-major)
- * An entry is needed once its block is full.  An entry outside [0, n_blocks)
+ * max_blocks * B is at most 2^30.  An entry is needed once its block is full.  An entry outside [0, n_blocks)
  * is no block: its tokens are neither written nor read, nor seen by the
  * attention.  lens[b] is at most max_blocks * B + B - 1 (tokens past that are
  * neither written, read nor seen) and a negative one counts as 0. */

@@ -1,0 +1,777 @@
+// Attention of the last tokens of each sequence over the 8-bit cache: the kernels.
+//
+// The G query heads of a kv head and the call's queries of a sequence are its rows
+// (row = query * G + head).  Keys come in steps of 64.  A wave computes S^T (64 keys x
+// 16 NT rows) = K Q^T and O^T (d x rows) += V^T P^T with 16x16x32 matrix instructions,
+// codes and probabilities as fp16 (8-bit codes are exact there).  The contraction index of
+// a product may be permuted if both operands agree: the rows of K are dealt to the four
+// 16-key tiles of a step such that the scores a lane holds (keys 16 g .. 16 g + 15, g =
+// lane / 16) are the keys of its V operand, 16 consecutive bytes of the channel-major V.
+// So probabilities never move between lanes.
+//
+// Scales: a lane's 16 keys lie in one block (B >= 16).  The scale of K goes with the factor
+// of the scores; that of V into the exponent of the probabilities, relative to the largest
+// of the wave's chunk of blocks (2^7 at most, so that small blocks keep their bits in fp16),
+// and out of the sums again by one product a step.
+//
+// Few rows (attn8_kernel): HBM-bound; the waves of a workgroup take runs of steps of their
+// own, operands straight from global memory, and meet in LDS at the end; where a call has
+// few tiles, several workgroups share a tile's keys and a second launch joins them.
+// Many rows (attn8_tile_kernel): bound by the matrix cores and what feeds them; four waves of
+// 32 rows share each step's keys and values, widened to fp16 once into LDS.
+#pragma once
+#include <math.h>
+
+#include "kvb_device.h"
+#include "kvb_internal.h"
+
+namespace kvb {
+namespace {
+
+typedef __attribute__((ext_vector_type(2))) _Float16 half2_t;
+typedef __attribute__((ext_vector_type(8))) _Float16 half8_t;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf8_t;
+typedef __attribute__((ext_vector_type(4))) float f4_t;
+typedef __attribute__((ext_vector_type(2))) float f2_t;
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kNoMax = -1e30f;  // running maximum before the first visible key
+constexpr float kSlack = 8.f;     // the running maximum follows once it is off by 2^8
+constexpr int kScaleTop = 6;      // weights of V scales stay below 2^(kScaleTop + 1)
+constexpr int kWaves = 4;
+constexpr int kFewRows = 64;     // up to here a tile is one wave's rows
+constexpr int kFewSplits = 8;    // up to here a row's splits are joined one after another
+
+// four codes -> four fp16 numbers
+template <int CODE>
+__device__ __forceinline__ void widen4(uint32_t w, half2_t& a, half2_t& b) {
+  if constexpr (CODE == KVB_I8) {
+    // byte u = code + 128 under the exponent of 1024: the number 1024 + u
+    w ^= 0x80808080u;
+    const half2_t off = {(_Float16)-1152.f, (_Float16)-1152.f};
+    a = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, w, 0x04010400u)) + off;
+    b = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, w, 0x04030402u)) + off;
+  } else {
+    a = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, false));
+    b = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, true));
+  }
+}
+template <int CODE>
+__device__ __forceinline__ half8_t widen8(uint32_t w0, uint32_t w1) {
+  half2_t r[4];
+  widen4<CODE>(w0, r[0], r[1]);
+  widen4<CODE>(w1, r[2], r[3]);
+  return __builtin_bit_cast(half8_t, r);
+}
+
+// x combined over the lanes l, l ^ 16, l ^ 32 and l ^ 48; all four end with the result
+template <typename F>
+__device__ __forceinline__ float over4groups(float x, F f) {
+  const uint32_t u = __float_as_uint(x);
+  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const uint32_t v = __float_as_uint(f(__uint_as_float(a[0]), __uint_as_float(a[1])));
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float max4groups(float x) {
+  return over4groups(x, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ __forceinline__ float sum4groups(float x) {
+  return over4groups(x, [](float a, float b) { return a + b; });
+}
+
+// A sequence as the call sees it (32 bits: lens are int32, keys at most 2^31 - 1).
+struct Seq {
+  int n_q;   // its queries; 0 when cu_q does not fit the call
+  int q0;    // the first of them
+  int len;   // its tokens
+  int full;  // full blocks
+  int keys;  // tokens that can be seen
+};
+template <int B>
+__device__ __forceinline__ Seq seq_of(const Attn8& a, int b) {
+  Seq s;
+  s.q0 = a.cu_q[b];
+  const int64_t end = a.cu_q[b + 1];
+  s.n_q = s.q0 >= 0 && end > s.q0 && end <= a.n_queries ? (int)(end - s.q0) : 0;
+  s.len = max(a.c.lens[b], 0);
+  s.full = s.len / B;
+  s.keys = s.len;
+  if (s.full > a.c.max_blocks) s.full = a.c.max_blocks, s.keys = s.full * B;
+  return s;
+}
+// keys that query i of the sequence sees
+__device__ __forceinline__ int seen_by(const Seq& s, int i) {
+  return max(min(s.len - s.n_q + i + 1, s.keys), 0);
+}
+// the 64-key steps over full blocks that a tile needs; `last`: the tile's last query
+template <int B>
+__device__ __forceinline__ int steps_of(const Seq& s, int last) {
+  const int coded = min(seen_by(s, min(last, s.n_q - 1)), s.full * B);
+  return coded / 64 + (coded % 64 != 0);
+}
+
+// x of lane i: uniform (on the scalar unit), or a lane's own choice
+template <bool UNIFORM>
+__device__ __forceinline__ float lane_of(float x, int i) {
+  if constexpr (UNIFORM) return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), i));
+  return __shfl(x, i, 64);
+}
+__device__ __forceinline__ float max64(float x) {
+#pragma unroll
+  for (int k = 1; k < 16; k <<= 1) x = fmaxf(x, __shfl_xor(x, k, 64));
+  return max4groups(x);
+}
+
+// One row's result: x / sum in bfloat16, and the log of the sum.
+__device__ __forceinline__ void write_row(const Attn8& a, int q, int head, int D, int c, f4_t x,
+                                          float top, float sum) {
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  const int64_t r = (int64_t)q * a.n_q_heads + head;
+  *reinterpret_cast<uint2*>(a.out + r * D + c) =
+      make_uint2(pack_bf16x2(x[0] * inv, x[1] * inv), pack_bf16x2(x[2] * inv, x[3] * inv));
+  if (a.lse && c == 0) a.lse[r] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+}
+
+// The state of a wave: its rows' queries, running maxima and sums, and outputs O^T in units
+// of 2^(vexp - kScaleTop).
+template <int D, int B, int NT, bool WEIGHTS>
+struct Rows {
+  static constexpr int KS = D / 32;           // contraction steps of a score
+  static constexpr int CT = D / 16;           // channel tiles of the output
+  static constexpr int PB = B < 64 ? B : 64;  // tokens of a part with a weight of its own
+  half8_t q[NT][KS];
+  float cq[NT];              // score (log2 units) of a product: cq * scale of K
+  int see[NT];               // keys the row sees
+  const uint16_t* qrow[NT];
+  float m[NT], l[NT];
+  f4_t o[NT][CT];
+  int vexp;
+  float* parts;  // log2 weights of the parts, of plan.rows rows each
+  int n_parts;   // the parts below this are written
+  int row, rows; // this lane's first row (the others follow 16 apart), rows of a part
+
+  // Queries: a power of two brings each row's largest value into [0.5, 1), so that fp16 holds
+  // a bfloat16 of the row exactly (below 2^-14 of the largest: to 2^-25 of it).  They carry the
+  // sign of softmax_scale, so that the scores' factors are not negative.
+  __device__ __forceinline__ void start(const Attn8& a, const Seq& sq, int h, int G, int row0,
+                                        int grp, int col) {
+    const uint32_t flip = a.softmax_scale < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int r = row0 + n * 16 + col, i = (int)((unsigned)r / (unsigned)G);
+      const bool ok = i < sq.n_q;  // a row past the last one reads the first one and sees nothing
+      qrow[n] = a.q + ((int64_t)(sq.q0 + (ok ? i : 0)) * a.n_q_heads + h * G + (ok ? r - i * G : 0)) * D;
+      see[n] = ok ? seen_by(sq, i) : 0;
+      uint4 w[KS];
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+        w[k] = *reinterpret_cast<const uint4*>(qrow[n] + 64 * (k / 2) + 16 * grp + 8 * (k % 2));
+      uint32_t big = 0;  // the largest magnitude's bits: integers order like magnitudes
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        const uint32_t u[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          big = max(big, max(u[e] << 16 & 0x7FFF0000u, u[e] & 0x7FFF0000u));
+      }
+      const float top = over4groups(__uint_as_float(big), [](float x, float y) {
+        return __uint_as_float(max(__float_as_uint(x), __float_as_uint(y)));
+      });
+      const int e2 = top > 0.f && top < INFINITY ? __builtin_amdgcn_frexp_expf(top) : 0;
+      cq[n] = __builtin_ldexpf(fabsf(a.softmax_scale) * kLog2e, e2);
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        const uint32_t u[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          q[n][k][2 * e] = (_Float16)__builtin_ldexpf(bf16_lo(u[e] ^ flip), -e2);
+          q[n][k][2 * e + 1] = (_Float16)__builtin_ldexpf(bf16_hi(u[e] ^ flip), -e2);
+        }
+      }
+      m[n] = kNoMax, l[n] = 0.f;
+#pragma unroll
+      for (int c = 0; c < CT; ++c) o[n][c] = (f4_t){0.f, 0.f, 0.f, 0.f};
+    }
+    vexp = -127;
+  }
+
+  // room for scales of V up to `big`
+  __device__ __forceinline__ void fit(float big) {
+    if (big > 0.f) {
+      const int e = max(__builtin_amdgcn_frexp_expf(big), -100);
+      if (e > vexp) unit(e);
+    }
+  }
+  // outputs in units of 2^(e - kScaleTop) from here on
+  __device__ __forceinline__ void unit(int e) {
+    const float f = __builtin_ldexpf(1.f, vexp - e);
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int c = 0; c < CT; ++c) o[n][c] *= f;
+    vexp = e;
+  }
+
+  // Raw scores -> probabilities times 2^lv (the scale of V) of the step: exp2(f s - m + lv).  The
+  // running maximum, the sums (iv = 2^-lv takes the scale out again) and the part's weight
+  // follow.  f >= 0; masked scores are -infinity with f = 1.  key: the first of this lane's 16.
+  __device__ __forceinline__ void soften(int n, float (&s)[16], float f, float lv, float iv, int key) {
+    float top = s[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+    top = max4groups(top * f);
+    if (__any(top > m[n] + kSlack)) {
+      const float next = top > m[n] + kSlack ? top : m[n];
+      const float g = __builtin_amdgcn_exp2f(m[n] - next);
+      l[n] *= g;
+#pragma unroll
+      for (int c = 0; c < CT; ++c) o[n][c] *= g;
+      m[n] = next;
+    }
+    const float bias = lv - m[n];
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], f, bias));
+      sum += s[i];
+    }
+    sum *= iv;
+    l[n] += sum;
+    if constexpr (WEIGHTS) {
+      if constexpr (PB == 32) {
+        const uint32_t u = __float_as_uint(sum);
+        const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+        sum = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+      }
+      if constexpr (PB == 64) sum = sum4groups(sum);
+      if (key % PB == 0) put_part(n, key / PB, m[n] + __builtin_amdgcn_logf(sum));
+    }
+  }
+
+  // Scores of a step of coded keys -> the operand of the product with V.  lv, iv, nan: log2 of the
+  // scale of V in the outputs' unit, its reciprocal, and whether it is a NaN (this lane's block).
+  __device__ __forceinline__ void step(float (&s)[NT][16], int key, bool have, float ks, float lv,
+                                       float iv, half8_t (&pr)[NT][2]) {
+    bool clear = have;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) clear = clear && see[n] >= key + 16;
+    const bool plain = __all(clear);  // every key of the step is seen by every row
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      float f = ks * cq[n];
+      if (!plain) {
+        const int left = have ? see[n] - key : 0;  // visible of the lane's 16 keys
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[n][i] = i < left ? s[n][i] * f : -INFINITY;
+        f = 1.f;
+      }
+      soften(n, s[n], f, lv, iv, key);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        half2_t x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const f2_t v = {s[n][8 * j + 2 * e], s[n][8 * j + 2 * e + 1]};
+          x[e] = __builtin_convertvector(v, half2_t);
+        }
+        pr[n][j] = __builtin_bit_cast(half8_t, x);
+      }
+    }
+  }
+  // A block of V whose scale is a NaN has codes 0: the rows that see of it (keys from `key` on) become
+  // NaN, the others stay clean.  The channels of a row lie in the four lanes of its column.
+  __device__ __forceinline__ void spoil(bool nan, int key) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const float x = sum4groups(nan && see[n] > key ? __builtin_nanf("") : 0.f);
+#pragma unroll
+      for (int c = 0; c < CT; ++c) o[n][c] += x;
+    }
+  }
+  // One step of 64 keys of the tail, bfloat16 rows from r0 on.  Probabilities enter as the sum of two
+  // bfloat16, in the outputs' unit; rows past the tail's end hold anything, so their values of V
+  // are cleared.
+  __device__ __forceinline__ void tail(const Attn8& a, const Seq& sq, int z, int r0, int lane) {
+    if (vexp < kScaleTop) unit(kScaleTop);  // 1 at least: the sums fit a float if the outputs do
+    const uint16_t* kt = a.c.k_tail + (int64_t)z * B * D;
+    const uint16_t* vt = a.c.v_tail + (int64_t)z * B * D;
+    const int grp = lane >> 4, col = lane & 15, t0 = sq.full * B + r0;
+    const int rows = min(64, sq.len - t0);  // tail rows of this step
+    float s[NT][16];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      f4_t acc[NT];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) acc[n] = (f4_t){0.f, 0.f, 0.f, 0.f};
+      // rows past the block are read like its last one; they are not seen
+      const int u = min(r0 + 16 * (col >> 2) + 4 * t + (col & 3), B - 1);
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        const bf8_t x = *reinterpret_cast<const bf8_t*>(kt + u * D + k * 32 + grp * 8);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const bf8_t y = *reinterpret_cast<const bf8_t*>(qrow[n] + k * 32 + grp * 8);
+          acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, acc[n], 0, 0, 0);
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[n][4 * t + i] = acc[n][i];
+    }
+    bf8_t ph[NT][2], pl[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const float f = a.softmax_scale * kLog2e;
+      const int left = see[n] - (t0 + 16 * grp);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[n][i] = i < left ? s[n][i] * f : -INFINITY;
+      soften(n, s[n], 1.f, 0.f, 1.f, t0 + 16 * grp);
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float p = __builtin_ldexpf(s[n][8 * j + e], kScaleTop - vexp);
+          const __bf16 top = (__bf16)p;
+          ph[n][j][e] = top;
+          pl[n][j][e] = (__bf16)(p - (float)top);
+        }
+    }
+    uint32_t odd = 0;  // not 0: an infinity or NaN among the values of V
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int u = 16 * grp + 8 * j, at = min(r0 + u, B - 8);
+      uint32_t in[4];  // the halves of each word that are rows of the tail
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        in[e] = (u + 2 * e < rows ? 0xFFFFu : 0u) | (u + 2 * e + 1 < rows ? 0xFFFF0000u : 0u);
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
+        const uint4 x = *reinterpret_cast<const uint4*>(vt + (c * 16 + col) * B + at);
+        uint32_t w[4] = {x.x & in[0], x.y & in[1], x.z & in[2], x.w & in[3]};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t bad = ((w[e] & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) |
+                               ((w[e] & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
+          odd |= bad;
+          w[e] &= ~bad;
+        }
+        const bf8_t v = __builtin_bit_cast(bf8_t, make_uint4(w[0], w[1], w[2], w[3]));
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          o[n][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, ph[n][j], o[n][c], 0, 0, 0);
+          o[n][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pl[n][j], o[n][c], 0, 0, 0);
+        }
+      }
+    }
+    // infinities and NaN of V reach only the rows that see their token (0 * infinity must not): they
+    // stayed out of the products and are added one by one
+    if (__builtin_expect(__any(odd != 0), 0)) {
+      for (int u = 0; u < rows; ++u) {
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t bits = vt[(c * 16 + grp * 4 + i) * B + r0 + u];
+            const bool bad = (bits & 0x7F80u) == 0x7F80u;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+              if (bad && t0 + u < see[n]) o[n][c][i] += __uint_as_float(bits << 16);
+          }
+      }
+    }
+  }
+  // log2 of the weight of part p
+  __device__ __forceinline__ void put_part(int n, int p, float x) {
+    if (row + 16 * n < rows && p < n_parts) parts[(int64_t)p * rows + row + 16 * n] = x;
+  }
+};
+
+template <int D, int B, int CODE, int NT, bool WEIGHTS>
+__global__ void __launch_bounds__(64 * kWaves, 2)
+attn8_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __restrict__ ml,
+             float* __restrict__ parts) {
+  typedef Rows<D, B, NT, WEIGHTS> R;
+  constexpr int CT = R::CT;
+  constexpr int KP = D / 64;              // 16-byte pieces of a lane's key
+  constexpr int CHUNK = B < 64 ? B : 64;  // steps whose blocks' ids and scales a wave holds
+  constexpr bool ONE = B >= 64;           // a step lies in one block
+  constexpr int LDO = D + 4;
+  __shared__ __align__(16) float part_o[kWaves][16 * NT][LDO];
+  __shared__ float part_ml[kWaves][16 * NT][2];
+
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int grp = lane >> 4, col = lane & 15;
+  const int z = blockIdx.z, split = blockIdx.x;
+  const int b = z / a.c.n_kv_heads, h = z - b * a.c.n_kv_heads;
+  const int G = plan.group;
+  const int row0 = blockIdx.y * (16 * NT);
+  const int32_t* table = a.c.table + (int64_t)z * a.c.max_blocks;
+
+  // The wave's steps: the split's, divided evenly; the last split takes what is left over where a
+  // sequence is longer than the call was sized for.  The first ids are asked for before the
+  // sequence's length is known.
+  const int lo = split * plan.span + min(wave * plan.wave_span, plan.span);
+  int idn = -1;
+  {
+    const int blk = (ONE ? lo / (B / 64) : lo * (64 / B)) + lane;
+    if (blk < a.c.max_blocks) idn = table[blk];
+  }
+  const Seq sq = seq_of<B>(a, b);
+  if (row0 >= sq.n_q * G) return;
+  const int last = (int)((unsigned)(row0 + 16 * NT - 1) / (unsigned)G);
+  const int steps = steps_of<B>(sq, last);
+  if (split > 0 && split * plan.span >= steps) return;
+  int hi = min(min(lo + plan.wave_span, (split + 1) * plan.span), steps);
+  if (split == plan.n_splits - 1 && wave == kWaves - 1) hi = steps;
+
+  R r;
+  r.start(a, sq, h, G, row0, grp, col);
+  if constexpr (WEIGHTS) {
+    // parts of the full blocks; the tail's are its own wave's to write
+    r.parts = parts + (int64_t)z * plan.n_parts * plan.rows;
+    r.n_parts = sq.full * (B / R::PB), r.row = row0 + col, r.rows = plan.rows;
+  }
+
+  for (int c0 = lo; c0 < hi; c0 += CHUNK) {
+    const int c1 = min(c0 + CHUNK, hi);
+    const int blk0 = ONE ? c0 / (B / 64) : c0 * (64 / B);
+    // lane i holds id and scales of block blk0 + i
+    int id = idn;
+    if (c0 != lo) id = blk0 + lane < a.c.max_blocks ? table[blk0 + lane] : -1;
+    const uint64_t found = __ballot(blk0 + lane < sq.full && id >= 0 && id < a.c.n_blocks);
+    if (found == 0) {  // none of them is a block
+      if constexpr (WEIGHTS) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          for (int x = grp; x < (c1 - c0) * (64 / R::PB); x += 4)
+            r.put_part(n, c0 * (64 / R::PB) + x, -INFINITY);
+      }
+      continue;
+    }
+    // what is no block is read like the first one that is: no value of V may be a NaN
+    const bool mine = found >> lane & 1;
+    id = mine ? id : __builtin_amdgcn_readlane(id, __builtin_ctzll(found));
+    const float ks = a.c.k_scale[id], vs = mine ? a.c.v_scale[id] : 0.f;
+
+    uint4 kw[4][KP], vr[CT];
+    // the block of this lane's K row (keys 16 (col / 4) ..) or of its 16 keys (16 grp ..)
+    auto id_at = [&](int st, int sub) {
+      const int i = ONE ? st / (B / 64) - blk0 : st * (64 / B) + sub / (B / 16) - blk0;
+      return ONE ? __builtin_amdgcn_readlane(id, i) : __shfl(id, i, 64);
+    };
+    auto load_k = [&](int st) {
+      const int i = id_at(st, col >> 2);
+      const int in = ONE ? st % (B / 64) * 64 + 16 * (col >> 2) : 16 * (col >> 2) % B;
+      const uint8_t* p = a.c.k_codes + (int64_t)i * (B * D) + (in + (col & 3)) * D + grp * 16;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int x = 0; x < KP; ++x) kw[t][x] = *reinterpret_cast<const uint4*>(p + 4 * t * D + x * 64);
+    };
+    auto load_v = [&](int st) {
+      const int i = id_at(st, grp);
+      const int in = ONE ? st % (B / 64) * 64 + 16 * grp : 16 * grp % B;
+      const uint8_t* p = a.c.v_codes + (int64_t)i * (B * D) + col * B + in;
+#pragma unroll
+      for (int c = 0; c < CT; ++c) vr[c] = *reinterpret_cast<const uint4*>(p + c * 16 * B);
+    };
+    load_k(c0);
+    load_v(c0);
+    r.fit(max64(vs));
+    // 2^lv is the scale in the outputs' unit; a block of zeros or NaN has codes 0, any scale will do
+    const bool none = !(vs > 0.f);
+    const float vw = none ? 1.f : __builtin_ldexpf(vs, kScaleTop - r.vexp);
+    const float lv = __builtin_amdgcn_logf(vw), iv = 1.f / vw;
+    const uint64_t nans = __ballot(vs != vs);
+
+#pragma unroll 1
+    for (int st = c0; st < c1; ++st) {
+      const int key0 = st * 64;
+      const int gb = ONE ? st / (B / 64) - blk0 : st * (64 / B) + grp / (B / 16) - blk0;
+      const bool have = found >> gb & 1;
+      const float ksg = lane_of<ONE>(ks, gb), lvg = lane_of<ONE>(lv, gb), ivg = lane_of<ONE>(iv, gb);
+      float s[NT][16];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        f4_t acc[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[n] = (f4_t){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int x = 0; x < KP; ++x) {
+          const half8_t k0 = widen8<CODE>(kw[t][x].x, kw[t][x].y);
+          const half8_t k1 = widen8<CODE>(kw[t][x].z, kw[t][x].w);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, r.q[n][2 * x], acc[n], 0, 0, 0);
+            acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, r.q[n][2 * x + 1], acc[n], 0, 0, 0);
+          }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[n][4 * t + i] = acc[n][i];
+      }
+      if (st + 1 < c1) load_k(st + 1);
+      half8_t pr[NT][2];
+      r.step(s, key0 + 16 * grp, have, ksg, lvg, ivg, pr);
+      if (__builtin_expect(nans != 0, 0)) r.spoil(nans >> gb & 1, key0 + 16 * grp);
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
+        const half8_t v0 = widen8<CODE>(vr[c].x, vr[c].y), v1 = widen8<CODE>(vr[c].z, vr[c].w);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          r.o[n][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pr[n][0], r.o[n][c], 0, 0, 0);
+          r.o[n][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pr[n][1], r.o[n][c], 0, 0, 0);
+        }
+      }
+      if (st + 1 < c1) load_v(st + 1);
+    }
+  }
+
+  // The tail, a step for each of the first split's last waves (a block has at most two)
+  const int r0 = (kWaves - 1 - wave) * 64;
+  if constexpr (WEIGHTS) r.n_parts += B / R::PB;
+  if (split == 0 && r0 < B && sq.full * B + r0 < seen_by(sq, min(last, sq.n_q - 1)))
+    r.tail(a, sq, z, r0, lane);
+
+  // the waves meet
+  const float unit = __builtin_ldexpf(1.f, r.vexp - kScaleTop);
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    r.l[n] = sum4groups(r.l[n]);
+    if (grp == 0) part_ml[wave][n * 16 + col][0] = r.m[n], part_ml[wave][n * 16 + col][1] = r.l[n];
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+      *reinterpret_cast<f4_t*>(&part_o[wave][n * 16 + col][c * 16 + grp * 4]) = r.o[n][c] * unit;
+  }
+  __syncthreads();
+  constexpr int LPR = D / 4;  // lanes of a row
+  const bool whole = plan.n_splits == 1;
+#pragma unroll 1
+  for (int p = threadIdx.x; p < 16 * NT * LPR; p += 64 * kWaves) {
+    const int rr = p / LPR, c = p % LPR * 4;
+    const int row = row0 + rr;
+    if (row >= sq.n_q * G || row >= plan.rows) continue;
+    float top = part_ml[0][rr][0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, part_ml[w][rr][0]);
+    float sum = 0.f;
+    f4_t x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = __builtin_amdgcn_exp2f(part_ml[w][rr][0] - top);
+      sum += f * part_ml[w][rr][1];
+      x += f * *reinterpret_cast<const f4_t*>(&part_o[w][rr][c]);
+    }
+    const int64_t rec = ((int64_t)z * plan.n_splits + split) * plan.rows + row;
+    if ((!whole || WEIGHTS) && c == 0) ml[2 * rec] = top, ml[2 * rec + 1] = sum;
+    if (!whole) {
+      *reinterpret_cast<f4_t*>(po + rec * D + c) = x;
+    } else {
+      const int i = (int)((unsigned)row / (unsigned)G);
+      write_row(a, sq.q0 + i, h * G + row - i * G, D, c, x, top, sum);
+    }
+  }
+}
+
+// Many rows: a workgroup takes 128 rows, 32 a wave.  Each step's codes are read once (a thread a
+// sixteenth of it ahead of the step before), widened to fp16 and shared through LDS, two steps'
+// room in turn.  K lies in rows of keys (in tile order), V in rows of channels; the 16-byte pieces
+// of a row are permuted by the row so that the 16 rows a matrix operand takes lie in all banks.
+template <int D, int B, int CODE, bool WEIGHTS>
+__global__ void __launch_bounds__(256, 2)
+attn8_tile_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __restrict__ ml,
+                  float* __restrict__ parts) {
+  constexpr int NT = 2;
+  typedef Rows<D, B, NT, WEIGHTS> R;
+  constexpr int KS = R::KS, CT = R::CT;
+  constexpr int CHUNK = B < 64 ? B : 64;
+  constexpr bool ONE = B >= 64;
+  constexpr int PC = D / 64;  // 16-byte pieces of codes of K, and of V, a thread takes of a step
+  constexpr int KC = D / 8;   // 16-byte pieces of a key's fp16 row
+  __shared__ __align__(16) half8_t kl[2][64 * KC], vl[2][D * 8];
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int grp = lane >> 4, col = lane & 15;
+  const int z = blockIdx.z, split = blockIdx.x;
+  const int b = z / a.c.n_kv_heads, h = z - b * a.c.n_kv_heads;
+  const int G = plan.group;
+  const int row0 = blockIdx.y * 128;
+  const int32_t* table = a.c.table + (int64_t)z * a.c.max_blocks;
+  const Seq sq = seq_of<B>(a, b);
+  if (row0 >= sq.n_q * G) return;
+  const int last = min((int)((unsigned)(row0 + 127) / (unsigned)G), sq.n_q - 1);
+  const int steps = steps_of<B>(sq, last);
+  const int lo = split * plan.span;
+  if (split > 0 && lo >= steps) return;
+  const int hi = split == plan.n_splits - 1 ? steps : min(lo + plan.span, steps);
+
+  R r;
+  const int wrow0 = row0 + 32 * wave;
+  r.start(a, sq, h, G, wrow0, grp, col);
+  if constexpr (WEIGHTS) {
+    r.parts = parts + (int64_t)z * plan.n_parts * plan.rows;
+    r.n_parts = sq.full * (B / R::PB), r.row = wrow0 + col, r.rows = plan.rows;
+  }
+
+  for (int c0 = lo; c0 < hi; c0 += CHUNK) {
+    const int c1 = min(c0 + CHUNK, hi);
+    const int blk0 = ONE ? c0 / (B / 64) : c0 * (64 / B);
+    int id = blk0 + lane < a.c.max_blocks ? table[blk0 + lane] : -1;
+    const uint64_t found = __ballot(blk0 + lane < sq.full && id >= 0 && id < a.c.n_blocks);
+    if (found == 0) {  // none of them is a block
+      if constexpr (WEIGHTS) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          for (int x = grp; x < (c1 - c0) * (64 / R::PB); x += 4)
+            r.put_part(n, c0 * (64 / R::PB) + x, -INFINITY);
+      }
+      continue;
+    }
+    const bool mine = found >> lane & 1;
+    id = mine ? id : __builtin_amdgcn_readlane(id, __builtin_ctzll(found));
+    const float ks = a.c.k_scale[id], vs = mine ? a.c.v_scale[id] : 0.f;
+
+    uint4 kw[PC], vw4[PC];
+    auto load = [&](int st) {
+#pragma unroll
+      for (int i = 0; i < PC; ++i) {
+        const int p = tid + 256 * i;
+        if constexpr (ONE) {
+          const int blk = __builtin_amdgcn_readlane(id, st / (B / 64) - blk0), sub = st % (B / 64);
+          kw[i] = *reinterpret_cast<const uint4*>(a.c.k_codes + (int64_t)blk * (B * D) + sub * 64 * D + p * 16);
+          vw4[i] = *reinterpret_cast<const uint4*>(a.c.v_codes + (int64_t)blk * (B * D) + sub * 64 +
+                                                   (p >> 2) * B + (p & 3) * 16);
+        } else {
+          const int key = p / (D / 16), kb = st * (64 / B) + key / B - blk0;
+          const int vb = st * (64 / B) + (p & 3) / (B / 16) - blk0;
+          const int64_t ki = __shfl(id, kb, 64), vi = __shfl(id, vb, 64);
+          kw[i] = *reinterpret_cast<const uint4*>(a.c.k_codes + ki * (B * D) + key % B * D + p % (D / 16) * 16);
+          vw4[i] = *reinterpret_cast<const uint4*>(a.c.v_codes + vi * (B * D) + (p >> 2) * B +
+                                                   (p & 3) % (B / 16) * 16);
+        }
+      }
+    };
+    auto store = [&](int buf) {
+#pragma unroll
+      for (int i = 0; i < PC; ++i) {
+        const int p = tid + 256 * i;
+        const int key = p / (D / 16), c = p % (D / 16) * 2;
+        const int row = (key & 12) * 4 + (key >> 4) * 4 + (key & 3);  // tile (key % 16) / 4, row of it
+        kl[buf][row * KC + (c ^ (row & (KC - 1)))] = widen8<CODE>(kw[i].x, kw[i].y);
+        kl[buf][row * KC + ((c + 1) ^ (row & (KC - 1)))] = widen8<CODE>(kw[i].z, kw[i].w);
+        const int ch = p >> 2, k = (p & 3) * 2;
+        vl[buf][ch * 8 + (k ^ (ch >> 1 & 7))] = widen8<CODE>(vw4[i].x, vw4[i].y);
+        vl[buf][ch * 8 + ((k + 1) ^ (ch >> 1 & 7))] = widen8<CODE>(vw4[i].z, vw4[i].w);
+      }
+    };
+    load(c0);
+    r.fit(max64(vs));
+    const bool none = !(vs > 0.f);
+    const float vw = none ? 1.f : __builtin_ldexpf(vs, kScaleTop - r.vexp);
+    const float lv = __builtin_amdgcn_logf(vw), iv = 1.f / vw;
+    const uint64_t nans = __ballot(vs != vs);
+    store(0);
+    if (c0 + 1 < c1) load(c0 + 1);
+    __syncthreads();
+
+#pragma unroll 1
+    for (int st = c0; st < c1; ++st) {
+      const int buf = (st - c0) & 1;
+      const int key0 = st * 64;
+      const int gb = ONE ? st / (B / 64) - blk0 : st * (64 / B) + grp / (B / 16) - blk0;
+      const bool have = found >> gb & 1;
+      const float ksg = lane_of<ONE>(ks, gb), lvg = lane_of<ONE>(lv, gb), ivg = lane_of<ONE>(iv, gb);
+      float s[NT][16];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        f4_t acc[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[n] = (f4_t){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+          const int row = t * 16 + col, c = 8 * (k / 2) + 2 * grp + k % 2;
+          const half8_t x = kl[buf][row * KC + (c ^ (row & (KC - 1)))];
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+            acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, r.q[n][k], acc[n], 0, 0, 0);
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[n][4 * t + i] = acc[n][i];
+      }
+      half8_t pr[NT][2];
+      r.step(s, key0 + 16 * grp, have, ksg, lvg, ivg, pr);
+      if (__builtin_expect(nans != 0, 0)) r.spoil(nans >> gb & 1, key0 + 16 * grp);
+      if (st + 1 < c1) store(buf ^ 1);
+      if (st + 2 < c1) load(st + 2);
+#pragma unroll
+      for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int ch = c * 16 + col;
+          const half8_t x = vl[buf][ch * 8 + ((2 * grp + j) ^ (ch >> 1 & 7))];
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+            r.o[n][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, pr[n][j], r.o[n][c], 0, 0, 0);
+        }
+      __syncthreads();
+    }
+  }
+
+  if constexpr (WEIGHTS) r.n_parts += B / R::PB;
+  if (split == 0)
+    for (int r0 = 0; r0 < B && sq.full * B + r0 < seen_by(sq, last); r0 += 64) r.tail(a, sq, z, r0, lane);
+
+  const float unit = __builtin_ldexpf(1.f, r.vexp - kScaleTop);
+  const bool whole = plan.n_splits == 1;
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int row = wrow0 + n * 16 + col;
+    const float sum = sum4groups(r.l[n]);
+    if (row >= sq.n_q * G || row >= plan.rows) continue;
+    const int64_t rec = ((int64_t)z * plan.n_splits + split) * plan.rows + row;
+    if ((!whole || WEIGHTS) && grp == 0) ml[2 * rec] = r.m[n], ml[2 * rec + 1] = sum;
+    const int i = (int)((unsigned)row / (unsigned)G);
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+      const int ch = c * 16 + grp * 4;
+      if (whole) write_row(a, sq.q0 + i, h * G + row - i * G, D, ch, r.o[n][c] * unit, r.m[n], sum);
+      else *reinterpret_cast<f4_t*>(po + rec * D + ch) = r.o[n][c] * unit;
+    }
+  }
+}
+
+template <int D, int B, int CODE>
+void launch_kernels(const Attn8Plan& plan, const Attn8& a, float* po, float* ml, float* parts,
+                    hipStream_t s) {
+  const dim3 grid((unsigned)plan.n_splits, (unsigned)plan.n_tiles, (unsigned)(a.c.n_seqs * a.c.n_kv_heads));
+#define KVB_ATTN(...) hipLaunchKernelGGL((__VA_ARGS__), grid, dim3(256), 0, s, a, plan, po, ml, parts)
+  const bool w = a.weights_out != nullptr;
+  if (plan.tile_rows == 16) {
+    if (w) KVB_ATTN(attn8_kernel<D, B, CODE, 1, true>);
+    else KVB_ATTN(attn8_kernel<D, B, CODE, 1, false>);
+  } else if (plan.tile_rows == 32) {
+    if (w) KVB_ATTN(attn8_kernel<D, B, CODE, 2, true>);
+    else KVB_ATTN(attn8_kernel<D, B, CODE, 2, false>);
+  } else {
+    if (w) KVB_ATTN(attn8_tile_kernel<D, B, CODE, true>);
+    else KVB_ATTN(attn8_tile_kernel<D, B, CODE, false>);
+  }
+#undef KVB_ATTN
+}
+
+template <int D, int CODE>
+void launch_kernels(const Attn8Plan& plan, const Attn8& a, int block_len, float* po, float* ml,
+                    float* parts, hipStream_t s) {
+  if (block_len == 16) launch_kernels<D, 16, CODE>(plan, a, po, ml, parts, s);
+  else if (block_len == 32) launch_kernels<D, 32, CODE>(plan, a, po, ml, parts, s);
+  else if (block_len == 64) launch_kernels<D, 64, CODE>(plan, a, po, ml, parts, s);
+  else launch_kernels<D, 128, CODE>(plan, a, po, ml, parts, s);
+}
+
+}  // namespace
+}  // namespace kvb

@@ -682,6 +682,7 @@ static kvb_status check_cache8(const kvb_cache8_layout* p, bool table_only = fal
   REQUIRE(p != nullptr, "layout is NULL");
   REQUIRE(p->n_kv_heads > 0 && p->block_len > 0 && p->max_blocks > 0,
           "cache layout has a non-positive size");
+  REQUIRE((int64_t)p->max_blocks * p->block_len <= (int64_t)1 << 30, "max_blocks * block_len > 2^30");
   if (table_only) return KVB_OK;
   REQUIRE(p->n_blocks > 0 && p->head_dim > 0, "cache layout has a non-positive size");
   if (kvb_status s = check_head_dim(p->head_dim)) return s;

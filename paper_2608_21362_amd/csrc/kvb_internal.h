@@ -155,13 +155,15 @@ hipError_t launch_cache8_evict(const Evict& a, int n_layers, hipStream_t s);
 
 // How a kvb_cache8_attn call is cut into workgroups, and its workspace.
 struct Attn8Plan {
-  int col_tiles;       // 16-query tiles of a wave (1 or 2)
-  int n_tiles;         // query tiles per (sequence, kv head)
+  int tile_rows;       // rows of a tile: 16 or 32 (few rows), 128 (many)
+  int n_tiles;         // tiles per (sequence, kv head)
   int n_splits;        // workgroups that share a tile's keys
   int span;            // 64-key steps of each but the last
   int wave_span;       // steps of a wave of it
   int group;           // query heads of a kv head
   int rows;            // query rows of a (sequence, kv head), at most
+  int join_wgs;        // workgroups of a (sequence, kv head) that join rows, and
+  int weight_wgs;      // that add weights, in the launch that follows
   int n_parts;         // parts of up to 64 tokens of a block with a weight of their own
   size_t ml_offset;    // (max, sum) of each (sequence, kv head, split, row)
   size_t parts_offset; // log2 weight of each (sequence, kv head, part, row)
@@ -179,6 +181,14 @@ struct Attn8 {
   const float* weights_in;
   float* weights_out;
 };
+void attn8_d64_i8(const Attn8Plan& plan, const Attn8& a, int block_len, float* po, float* ml, float* parts,
+                  hipStream_t s);
+void attn8_d64_e4m3(const Attn8Plan& plan, const Attn8& a, int block_len, float* po, float* ml,
+                    float* parts, hipStream_t s);
+void attn8_d128_i8(const Attn8Plan& plan, const Attn8& a, int block_len, float* po, float* ml,
+                   float* parts, hipStream_t s);
+void attn8_d128_e4m3(const Attn8Plan& plan, const Attn8& a, int block_len, float* po, float* ml,
+                     float* parts, hipStream_t s);
 hipError_t launch_cache8_attn(const Attn8Plan& plan, const Attn8& a, int head_dim, int block_len,
                               int code, void* workspace, hipStream_t s);
 

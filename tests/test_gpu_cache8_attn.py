@@ -211,7 +211,11 @@ def test_rows_that_see_none_of_a_block_stay_clean():
     ref, rlse, _ = attend(_kvb(), good, good.device(), q, [80])
     # both are within 2^-8 of the output and 2^-10 of the largest value of what is exact
     near = 2.0 ** -7 * ref[:16].float().abs() + 2.0 ** -9 * float(np.abs(v[:128]).max())
-    assert ((out[:16].float() - ref[:16].float()).abs() <= near).all() and torch.equal(lse[:16], rlse[:16])
+    assert ((out[:16].float() - ref[:16].float()).abs() <= near).all()
+    # the scale of V goes into the exponents relative to the other blocks' scales, so the two calls round other
+    # exponents: below 64, off by 2^-19 each; a sum of such powers, with their own roundings, by 2^-17 of itself;
+    # its logarithm by that and two roundings of the result, in each call
+    assert ((lse[:16] - rlse[:16]).abs() <= 2 * (2.0 ** -17 + 2.0 ** -23 * rlse[:16].abs())).all()
     assert torch.isnan(out[16:].float()).all() and torch.isnan(lse[16:]).all()
 
 
