@@ -158,12 +158,14 @@ Attn8Plan attn8_plan(int n_kv_heads, int head_dim, int block_len, int max_blocks
   Attn8Plan p{};
   p.group = n_q_heads / n_kv_heads;
   p.rows = max_queries * p.group;
-  p.tile_rows = p.rows <= 16 ? 16 : p.rows <= kFewRows ? 32 : 128;
+  p.tile_rows = p.rows <= 16 ? 16 : p.rows <= kFewRows ? 32 : kManyTile;
   p.n_tiles = (p.rows + p.tile_rows - 1) / p.tile_rows;
   const int64_t heads = (int64_t)n_seqs * n_kv_heads, base = heads * p.n_tiles;
   const int64_t steps = ((int64_t)max_len + 63) / 64;
-  // enough workgroups to fill 256 CUs twice, each with two steps a wave at least
-  int64_t want = (512 + base - 1) / base, most = steps / 8;
+  // few rows: enough workgroups to fill 256 CUs twice, each with two steps a wave at least; many
+  // rows: a workgroup a CU, of 16 steps at least
+  const bool few = p.tile_rows != kManyTile;
+  int64_t want = ((few ? 512 : 256) + base - 1) / base, most = steps / (few ? 8 : 16);
   if (want > most) want = most;
   if (want < 1) want = 1;
   if (want > 256) want = 256;  // what the join takes

@@ -40,6 +40,7 @@ constexpr float kSlack = 8.f;     // the running maximum follows once it is off 
 constexpr int kScaleTop = 6;      // weights of V scales stay below 2^(kScaleTop + 1)
 constexpr int kWaves = 4;
 constexpr int kFewRows = 64;     // up to here a tile is one wave's rows
+constexpr int kManyTile = 256;   // rows of a tile beyond
 constexpr int kFewSplits = 8;    // up to here a row's splits are joined one after another
 
 // four codes -> four fp16 numbers
@@ -143,7 +144,6 @@ struct Rows {
   half8_t q[NT][KS];
   float cq[NT];              // score (log2 units) of a product: cq * scale of K
   int see[NT];               // keys the row sees
-  const uint16_t* qrow[NT];
   float m[NT], l[NT];
   f4_t o[NT][CT];
   int vexp;
@@ -154,19 +154,24 @@ struct Rows {
   // Queries: a power of two brings each row's largest value into [0.5, 1), so that fp16 holds
   // a bfloat16 of the row exactly (below 2^-14 of the largest: to 2^-25 of it).  They carry the
   // sign of softmax_scale, so that the scores' factors are not negative.
+  // where query row r lies; a row past the last one reads the first one (and sees nothing)
+  static __device__ __forceinline__ const uint16_t* query(const Attn8& a, const Seq& sq, int h, int G, int r) {
+    const int i = (int)((unsigned)r / (unsigned)G);
+    const bool ok = i < sq.n_q;
+    return a.q + ((int64_t)(sq.q0 + (ok ? i : 0)) * a.n_q_heads + h * G + (ok ? r - i * G : 0)) * D;
+  }
   __device__ __forceinline__ void start(const Attn8& a, const Seq& sq, int h, int G, int row0,
                                         int grp, int col) {
     const uint32_t flip = a.softmax_scale < 0.f ? 0x80008000u : 0u;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       const int r = row0 + n * 16 + col, i = (int)((unsigned)r / (unsigned)G);
-      const bool ok = i < sq.n_q;  // a row past the last one reads the first one and sees nothing
-      qrow[n] = a.q + ((int64_t)(sq.q0 + (ok ? i : 0)) * a.n_q_heads + h * G + (ok ? r - i * G : 0)) * D;
-      see[n] = ok ? seen_by(sq, i) : 0;
+      const uint16_t* qrow = query(a, sq, h, G, r);
+      see[n] = i < sq.n_q ? seen_by(sq, i) : 0;
       uint4 w[KS];
 #pragma unroll
       for (int k = 0; k < KS; ++k)
-        w[k] = *reinterpret_cast<const uint4*>(qrow[n] + 64 * (k / 2) + 16 * grp + 8 * (k % 2));
+        w[k] = *reinterpret_cast<const uint4*>(qrow + 64 * (k / 2) + 16 * grp + 8 * (k % 2));
       uint32_t big = 0;  // the largest magnitude's bits: integers order like magnitudes
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
@@ -292,7 +297,8 @@ struct Rows {
   // One step of 64 keys of the tail, bfloat16 rows from r0 on.  Probabilities enter as the sum of two
   // bfloat16, in the outputs' unit; rows past the tail's end hold anything, so their values of V
   // are cleared.
-  __device__ __forceinline__ void tail(const Attn8& a, const Seq& sq, int z, int r0, int lane) {
+  __device__ __forceinline__ void tail(const Attn8& a, const Seq& sq, int z, int h, int G, int row0, int r0,
+                                       int lane) {
     if (vexp < kScaleTop) unit(kScaleTop);  // 1 at least: the sums fit a float if the outputs do
     const uint16_t* kt = a.c.k_tail + (int64_t)z * B * D;
     const uint16_t* vt = a.c.v_tail + (int64_t)z * B * D;
@@ -311,7 +317,7 @@ struct Rows {
         const bf8_t x = *reinterpret_cast<const bf8_t*>(kt + u * D + k * 32 + grp * 8);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          const bf8_t y = *reinterpret_cast<const bf8_t*>(qrow[n] + k * 32 + grp * 8);
+          const bf8_t y = *reinterpret_cast<const bf8_t*>(query(a, sq, h, G, row0 + n * 16 + col) + k * 32 + grp * 8);
           acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, acc[n], 0, 0, 0);
         }
       }
@@ -534,7 +540,7 @@ attn8_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __restrict_
   const int r0 = (kWaves - 1 - wave) * 64;
   if constexpr (WEIGHTS) r.n_parts += B / R::PB;
   if (split == 0 && r0 < B && sq.full * B + r0 < seen_by(sq, min(last, sq.n_q - 1)))
-    r.tail(a, sq, z, r0, lane);
+    r.tail(a, sq, z, h, G, row0, r0, lane);
 
   // the waves meet
   const float unit = __builtin_ldexpf(1.f, r.vexp - kScaleTop);
@@ -576,33 +582,64 @@ attn8_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __restrict_
   }
 }
 
-// Many rows: a workgroup takes 128 rows, 32 a wave.  Each step's codes are read once (a thread a
-// sixteenth of it ahead of the step before), widened to fp16 and shared through LDS, two steps'
-// room in turn.  K lies in rows of keys (in tile order), V in rows of channels; the 16-byte pieces
-// of a row are permuted by the row so that the 16 rows a matrix operand takes lie in all banks.
+// The ids and scales of 64 blocks (or fewer: `steps` 64-key steps from step0 on), one a lane.
+template <int B>
+struct Chunk {
+  static constexpr int STEPS = B < 64 ? B : 64;
+  static constexpr bool ONE = B >= 64;  // a step lies in one block
+  int id, blk0;
+  uint64_t found;  // lanes whose entry is a block; the others read like the first one that is
+  __device__ __forceinline__ void load(const Attn8& a, const Seq& sq, const int32_t* table, int step0,
+                                       int lane) {
+    blk0 = ONE ? step0 / (B / 64) : step0 * (64 / B);
+    id = blk0 + lane < a.c.max_blocks ? table[blk0 + lane] : -1;
+    found = __ballot(blk0 + lane < sq.full && id >= 0 && id < a.c.n_blocks);
+    if (!(found >> lane & 1)) id = found ? __builtin_amdgcn_readlane(id, __builtin_ctzll(found)) : 0;
+  }
+  // the lane that holds the block of key group g (16 keys) of a step
+  __device__ __forceinline__ int lane_of_group(int st, int g) const {
+    return ONE ? st / (B / 64) - blk0 : st * (64 / B) + g / (B / 16) - blk0;
+  }
+  __device__ __forceinline__ int id_of_group(int st, int g) const {
+    return ONE ? __builtin_amdgcn_readlane(id, st / (B / 64) - blk0) : __shfl(id, lane_of_group(st, g), 64);
+  }
+};
+
+// Many rows: a workgroup takes 256 rows, 32 a wave, two waves a SIMD.  Each step's codes are read
+// once (a thread takes a 512th of it, two steps ahead), widened to fp16 and shared through LDS; K
+// lies in rows of keys (in tile order), V in rows of channels, and the 16-byte pieces of a row
+// are permuted by the row so that the 16 rows a matrix operand takes lie in all banks.
+//
+// The matrix cores and the vector unit of a SIMD work for one wave each: a wave's step is a run of
+// matrix products, M(i) = the product of step i - 1's probabilities with V, then the scores of step
+// i, and a run of vector work, S(i) = the probabilities of step i, codes of K (step i + 2) and of V
+// (i + 1) widened into LDS, loads of the next ones; waves 4 to 7 are one run behind waves 0 to 3,
+// and a barrier ends every run.  (With every wave free to run, 4 waves a workgroup and 2
+// workgroups a CU, both kinds of work took turns by chance: 887 TFLOP/s.)  Three slots: a slot is
+// written two runs before it is read and two runs after it was.
 template <int D, int B, int CODE, bool WEIGHTS>
-__global__ void __launch_bounds__(256, 2)
+__global__ void __launch_bounds__(512, 2)
 attn8_tile_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __restrict__ ml,
                   float* __restrict__ parts) {
   constexpr int NT = 2;
   typedef Rows<D, B, NT, WEIGHTS> R;
+  typedef Chunk<B> Ids;
   constexpr int KS = R::KS, CT = R::CT;
-  constexpr int CHUNK = B < 64 ? B : 64;
-  constexpr bool ONE = B >= 64;
-  constexpr int PC = D / 64;  // 16-byte pieces of codes of K, and of V, a thread takes of a step
-  constexpr int KC = D / 8;   // 16-byte pieces of a key's fp16 row
-  __shared__ __align__(16) half8_t kl[2][64 * KC], vl[2][D * 8];
+  constexpr bool ONE = Ids::ONE;
+  constexpr int KC = D / 8;          // 16-byte pieces of a key's fp16 row
+  constexpr int PIECES = 64 * D / 16;  // 16-byte pieces of codes of a step's K, and of its V
+  __shared__ __align__(16) half8_t kl[3][64 * KC], vl[3][D * 8];
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int grp = lane >> 4, col = lane & 15;
   const int z = blockIdx.z, split = blockIdx.x;
   const int b = z / a.c.n_kv_heads, h = z - b * a.c.n_kv_heads;
   const int G = plan.group;
-  const int row0 = blockIdx.y * 128;
+  const int row0 = blockIdx.y * kManyTile;
   const int32_t* table = a.c.table + (int64_t)z * a.c.max_blocks;
   const Seq sq = seq_of<B>(a, b);
   if (row0 >= sq.n_q * G) return;
-  const int last = min((int)((unsigned)(row0 + 127) / (unsigned)G), sq.n_q - 1);
+  const int last = min((int)((unsigned)(row0 + kManyTile - 1) / (unsigned)G), sq.n_q - 1);
   const int steps = steps_of<B>(sq, last);
   const int lo = split * plan.span;
   if (split > 0 && lo >= steps) return;
@@ -616,115 +653,158 @@ attn8_tile_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __rest
     r.n_parts = sq.full * (B / R::PB), r.row = wrow0 + col, r.rows = plan.rows;
   }
 
-  for (int c0 = lo; c0 < hi; c0 += CHUNK) {
-    const int c1 = min(c0 + CHUNK, hi);
-    const int blk0 = ONE ? c0 / (B / 64) : c0 * (64 / B);
-    int id = blk0 + lane < a.c.max_blocks ? table[blk0 + lane] : -1;
-    const uint64_t found = __ballot(blk0 + lane < sq.full && id >= 0 && id < a.c.n_blocks);
-    if (found == 0) {  // none of them is a block
-      if constexpr (WEIGHTS) {
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-          for (int x = grp; x < (c1 - c0) * (64 / R::PB); x += 4)
-            r.put_part(n, c0 * (64 / R::PB) + x, -INFINITY);
-      }
-      continue;
-    }
-    const bool mine = found >> lane & 1;
-    id = mine ? id : __builtin_amdgcn_readlane(id, __builtin_ctzll(found));
-    const float ks = a.c.k_scale[id], vs = mine ? a.c.v_scale[id] : 0.f;
-
-    uint4 kw[PC], vw4[PC];
-    auto load = [&](int st) {
-#pragma unroll
-      for (int i = 0; i < PC; ++i) {
-        const int p = tid + 256 * i;
-        if constexpr (ONE) {
-          const int blk = __builtin_amdgcn_readlane(id, st / (B / 64) - blk0), sub = st % (B / 64);
-          kw[i] = *reinterpret_cast<const uint4*>(a.c.k_codes + (int64_t)blk * (B * D) + sub * 64 * D + p * 16);
-          vw4[i] = *reinterpret_cast<const uint4*>(a.c.v_codes + (int64_t)blk * (B * D) + sub * 64 +
-                                                   (p >> 2) * B + (p & 3) * 16);
-        } else {
-          const int key = p / (D / 16), kb = st * (64 / B) + key / B - blk0;
-          const int vb = st * (64 / B) + (p & 3) / (B / 16) - blk0;
-          const int64_t ki = __shfl(id, kb, 64), vi = __shfl(id, vb, 64);
-          kw[i] = *reinterpret_cast<const uint4*>(a.c.k_codes + ki * (B * D) + key % B * D + p % (D / 16) * 16);
-          vw4[i] = *reinterpret_cast<const uint4*>(a.c.v_codes + vi * (B * D) + (p >> 2) * B +
-                                                   (p & 3) % (B / 16) * 16);
-        }
-      }
+  if (lo < hi) {
+    Ids ids[2];  // of the steps' current chunk and the next one
+    ids[0].load(a, sq, table, lo, lane);
+    ids[1].load(a, sq, table, lo + Ids::STEPS, lane);
+    int turn = lo + Ids::STEPS;  // the first step of the next chunk
+    float ks = 0.f, lv = 0.f, iv = 1.f;
+    uint64_t found = 0, nans = 0;
+    auto scales = [&]() {  // of the current chunk
+      found = ids[0].found;
+      ks = a.c.k_scale[ids[0].id];
+      const float vs = found >> lane & 1 ? a.c.v_scale[ids[0].id] : 0.f;
+      r.fit(max64(vs));
+      // 2^lv is the scale in the outputs' unit; a block of zeros or NaN has codes 0, any scale will do
+      const float vw = vs > 0.f ? __builtin_ldexpf(vs, kScaleTop - r.vexp) : 1.f;
+      lv = __builtin_amdgcn_logf(vw), iv = 1.f / vw;
+      nans = __ballot(vs != vs);
     };
-    auto store = [&](int buf) {
-#pragma unroll
-      for (int i = 0; i < PC; ++i) {
-        const int p = tid + 256 * i;
-        const int key = p / (D / 16), c = p % (D / 16) * 2;
-        const int row = (key & 12) * 4 + (key >> 4) * 4 + (key & 3);  // tile (key % 16) / 4, row of it
-        kl[buf][row * KC + (c ^ (row & (KC - 1)))] = widen8<CODE>(kw[i].x, kw[i].y);
-        kl[buf][row * KC + ((c + 1) ^ (row & (KC - 1)))] = widen8<CODE>(kw[i].z, kw[i].w);
-        const int ch = p >> 2, k = (p & 3) * 2;
-        vl[buf][ch * 8 + (k ^ (ch >> 1 & 7))] = widen8<CODE>(vw4[i].x, vw4[i].y);
-        vl[buf][ch * 8 + ((k + 1) ^ (ch >> 1 & 7))] = widen8<CODE>(vw4[i].z, vw4[i].w);
-      }
-    };
-    load(c0);
-    r.fit(max64(vs));
-    const bool none = !(vs > 0.f);
-    const float vw = none ? 1.f : __builtin_ldexpf(vs, kScaleTop - r.vexp);
-    const float lv = __builtin_amdgcn_logf(vw), iv = 1.f / vw;
-    const uint64_t nans = __ballot(vs != vs);
-    store(0);
-    if (c0 + 1 < c1) load(c0 + 1);
-    __syncthreads();
+    scales();
 
-#pragma unroll 1
-    for (int st = c0; st < c1; ++st) {
-      const int buf = (st - c0) & 1;
-      const int key0 = st * 64;
-      const int gb = ONE ? st / (B / 64) - blk0 : st * (64 / B) + grp / (B / 16) - blk0;
-      const bool have = found >> gb & 1;
-      const float ksg = lane_of<ONE>(ks, gb), lvg = lane_of<ONE>(lv, gb), ivg = lane_of<ONE>(iv, gb);
-      float s[NT][16];
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        f4_t acc[NT];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) acc[n] = (f4_t){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int k = 0; k < KS; ++k) {
-          const int row = t * 16 + col, c = 8 * (k / 2) + 2 * grp + k % 2;
-          const half8_t x = kl[buf][row * KC + (c ^ (row & (KC - 1)))];
-#pragma unroll
-          for (int n = 0; n < NT; ++n)
-            acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, r.q[n][k], acc[n], 0, 0, 0);
-        }
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) s[n][4 * t + i] = acc[n][i];
-      }
-      half8_t pr[NT][2];
-      r.step(s, key0 + 16 * grp, have, ksg, lvg, ivg, pr);
-      if (__builtin_expect(nans != 0, 0)) r.spoil(nans >> gb & 1, key0 + 16 * grp);
-      if (st + 1 < c1) store(buf ^ 1);
-      if (st + 2 < c1) load(st + 2);
-#pragma unroll
-      for (int c = 0; c < CT; ++c)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int ch = c * 16 + col;
-          const half8_t x = vl[buf][ch * 8 + ((2 * grp + j) ^ (ch >> 1 & 7))];
-#pragma unroll
-          for (int n = 0; n < NT; ++n)
-            r.o[n][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, pr[n][j], r.o[n][c], 0, 0, 0);
-        }
+    // A thread's pieces of a step's K and V (head size 64: two threads a piece).  No branches: a step past
+    // the last one reads the last one, and lands in a slot that nobody reads.
+    uint4 kw[2], vw4[2];  // two steps' codes in flight
+    const int p = PIECES >= 512 ? tid : tid & (PIECES - 1);
+    const int key = p / (D / 16), kc = p % (D / 16) * 2, ch = p >> 2, vk = (p & 3) * 2;
+    const int krow = (key & 12) * 4 + (key >> 4) * 4 + (key & 3);  // tile (key % 16) / 4, row of it
+    auto block_of = [&](int st, int group) {
+      const bool next = st >= turn;
+      const int id = next ? ids[1].id : ids[0].id, blk0 = next ? ids[1].blk0 : ids[0].blk0;
+      if constexpr (ONE) return __builtin_amdgcn_readlane(id, st / (B / 64) - blk0);
+      else return __shfl(id, st * (64 / B) + group / (B / 16) - blk0, 64);
+    };
+    auto load_k = [&](int st, uint4& kw) {
+      st = min(st, hi - 1);
+      const int in = ONE ? st % (B / 64) * 64 + key : key % B;
+      kw = *reinterpret_cast<const uint4*>(a.c.k_codes + (int64_t)block_of(st, key >> 4) * (B * D) + in * D + kc * 8);
+    };
+    auto load_v = [&](int st, uint4& vw4) {
+      st = min(st, hi - 1);
+      const int in = ONE ? st % (B / 64) * 64 + vk * 8 : vk * 8 % B;
+      vw4 = *reinterpret_cast<const uint4*>(a.c.v_codes + (int64_t)block_of(st, p & 3) * (B * D) + ch * B + in);
+    };
+    const int k0 = krow * KC + (kc ^ (krow & (KC - 1))), k1 = krow * KC + ((kc + 1) ^ (krow & (KC - 1)));
+    const int v0 = ch * 8 + (vk ^ (ch >> 1 & 7)), v1 = ch * 8 + ((vk + 1) ^ (ch >> 1 & 7));
+    auto store_k = [&](int slot, const uint4& kw) {
+      half8_t* to = kl[0] + slot * (64 * KC);
+      to[k0] = widen8<CODE>(kw.x, kw.y);
+      to[k1] = widen8<CODE>(kw.z, kw.w);
+    };
+    auto store_v = [&](int st, int slot, const uint4& vw4) {
+      // no block at all in the chunk: no value of V may be a NaN
+      const uint32_t some = (st >= turn ? ids[1].found : ids[0].found) ? ~0u : 0u;
+      half8_t* to = vl[0] + slot * (D * 8);
+      to[v0] = widen8<CODE>(vw4.x & some, vw4.y & some);
+      to[v1] = widen8<CODE>(vw4.z & some, vw4.w & some);
+    };
+    auto run_ends = [&]() {
+      __builtin_amdgcn_sched_barrier(0);
       __syncthreads();
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    float s[NT][16];
+    half8_t pr[NT][2];
+    // where this lane's operand pieces lie in a slot: of contraction step k, and of keys 16 grp + 8 j ..
+    int ko[KS], vo[2];
+#pragma unroll
+    for (int k = 0; k < KS; ++k) ko[k] = col * KC + ((8 * (k / 2) + 2 * grp + k % 2) ^ (col & (KC - 1)));
+#pragma unroll
+    for (int j = 0; j < 2; ++j) vo[j] = col * 8 + ((2 * grp + j) ^ (col >> 1));
+    // A run of matrix products: V of the slot before (not for the first), then scores of slot `at`.  The
+    // operand pieces are read AHEAD of their products, in this order.
+    auto products = [&](int before, int at, bool first) {
+      constexpr int AHEAD = 6, NV = 2 * CT, ALL = NV + 4 * KS;
+      half8_t x[8];
+      f4_t acc[NT][4];
+      const half8_t* vp = vl[0] + before * (D * 8);
+      const half8_t* kp = kl[0] + at * (64 * KC);
+      auto piece = [&](int i) {
+        return i < NV ? vp[vo[i / CT] + i % CT * 128] : kp[ko[(i - NV) / 4] + (i - NV) % 4 * 16 * KC];
+      };
+      const int from = first ? NV : 0;
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) x[(from + i) % 8] = piece(from + i);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = from; i < ALL; ++i) {
+        if (i + AHEAD < ALL) x[(i + AHEAD) % 8] = piece(i + AHEAD);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          if (i < NV) {
+            r.o[n][i % CT] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[i % 8], pr[n][i / CT], r.o[n][i % CT], 0, 0, 0);
+          } else {
+            const int k = (i - NV) / 4, t = (i - NV) % 4;
+            acc[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+                x[i % 8], r.q[n][k], k == 0 ? (f4_t){0.f, 0.f, 0.f, 0.f} : acc[n][t], 0, 0, 0);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[n][e] = acc[n][e / 4][e % 4];
+    };
+
+    load_k(lo, kw[0]);
+    load_v(lo, vw4[0]);
+    load_k(lo + 1, kw[1]);
+    store_k(0, kw[0]);
+    store_v(lo, 0, vw4[0]);
+    load_k(lo + 2, kw[0]);
+    load_v(lo + 1, vw4[0]);
+    store_k(1, kw[1]);
+    load_k(lo + 3, kw[1]);
+    load_v(lo + 2, vw4[1]);
+    run_ends();
+    if (wave >= 4) run_ends();
+    products(0, 0, true);
+    run_ends();
+    int s0 = 0, s1 = 1, s2 = 2;  // slots of steps st, st + 1, st + 2
+    auto step = [&](int st, uint4& kw, uint4& vw4) {
+      const int key = st * 64 + 16 * grp;
+      const int gb = ids[0].lane_of_group(st, grp);
+      r.step(s, key, found >> gb & 1, lane_of<ONE>(ks, gb), lane_of<ONE>(lv, gb), lane_of<ONE>(iv, gb), pr);
+      if (__builtin_expect(nans != 0, 0)) r.spoil(nans >> gb & 1, key);
+      store_k(s2, kw);
+      store_v(st + 1, s1, vw4);
+      load_k(st + 4, kw);
+      load_v(st + 3, vw4);
+      run_ends();
+      __builtin_amdgcn_s_setprio(1);
+      products(s0, s1, false);  // behind the last step: scores of what the slot holds, for nothing
+      __builtin_amdgcn_s_setprio(0);
+      if (st + 1 == turn) {  // the next chunk's blocks; st + 4 at most was asked of them so far
+        ids[0] = ids[1];
+        turn += Ids::STEPS;
+        ids[1].load(a, sq, table, turn, lane);
+        scales();
+      }
+      const int x = s0;
+      s0 = s1, s1 = s2, s2 = x;
+      if (st + 1 < hi || wave < 4) run_ends();
+    };
+#pragma unroll 1
+    for (int st = lo; st < hi; st += 2) {
+      step(st, kw[0], vw4[0]);
+      if (st + 1 < hi) step(st + 1, kw[1], vw4[1]);
     }
   }
 
   if constexpr (WEIGHTS) r.n_parts += B / R::PB;
   if (split == 0)
-    for (int r0 = 0; r0 < B && sq.full * B + r0 < seen_by(sq, last); r0 += 64) r.tail(a, sq, z, r0, lane);
+    for (int r0 = 0; r0 < B && sq.full * B + r0 < seen_by(sq, last); r0 += 64) r.tail(a, sq, z, h, G, wrow0, r0, lane);
 
   const float unit = __builtin_ldexpf(1.f, r.vexp - kScaleTop);
   const bool whole = plan.n_splits == 1;
@@ -749,7 +829,8 @@ template <int D, int B, int CODE>
 void launch_kernels(const Attn8Plan& plan, const Attn8& a, float* po, float* ml, float* parts,
                     hipStream_t s) {
   const dim3 grid((unsigned)plan.n_splits, (unsigned)plan.n_tiles, (unsigned)(a.c.n_seqs * a.c.n_kv_heads));
-#define KVB_ATTN(...) hipLaunchKernelGGL((__VA_ARGS__), grid, dim3(256), 0, s, a, plan, po, ml, parts)
+  const dim3 block(plan.tile_rows == kManyTile ? 512 : 64 * kWaves);
+#define KVB_ATTN(...) hipLaunchKernelGGL((__VA_ARGS__), grid, block, 0, s, a, plan, po, ml, parts)
   const bool w = a.weights_out != nullptr;
   if (plan.tile_rows == 16) {
     if (w) KVB_ATTN(attn8_kernel<D, B, CODE, 1, true>);
