@@ -695,7 +695,7 @@ attn8_tile_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __rest
       vw4 = *reinterpret_cast<const uint4*>(a.c.v_codes + (int64_t)block_of(st, p & 3) * (B * D) + ch * B + in);
     };
     const int k0 = krow * KC + (kc ^ (krow & (KC - 1))), k1 = krow * KC + ((kc + 1) ^ (krow & (KC - 1)));
-    const int v0 = ch * 8 + (vk ^ (ch >> 1 & 7)), v1 = ch * 8 + ((vk + 1) ^ (ch >> 1 & 7));
+    const int v0 = ch * 8 + ((p & 3) ^ (ch >> 1 & 7)), v1 = ch * 8 + (((p & 3) + 4) ^ (ch >> 1 & 7));
     auto store_k = [&](int slot, const uint4& kw) {
       half8_t* to = kl[0] + slot * (64 * KC);
       to[k0] = widen8<CODE>(kw.x, kw.y);
@@ -720,7 +720,7 @@ attn8_tile_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __rest
 #pragma unroll
     for (int k = 0; k < KS; ++k) ko[k] = col * KC + ((8 * (k / 2) + 2 * grp + k % 2) ^ (col & (KC - 1)));
 #pragma unroll
-    for (int j = 0; j < 2; ++j) vo[j] = col * 8 + ((2 * grp + j) ^ (col >> 1));
+    for (int j = 0; j < 2; ++j) vo[j] = col * 8 + ((4 * j + grp) ^ (col >> 1));
     // A run of matrix products: V of the slot before (not for the first), then scores of slot `at`.  The
     // operand pieces are read AHEAD of their products, in this order.
     auto products = [&](int before, int at, bool first) {
