@@ -162,15 +162,16 @@ Attn8Plan attn8_plan(int n_kv_heads, int head_dim, int block_len, int max_blocks
   p.n_tiles = (p.rows + p.tile_rows - 1) / p.tile_rows;
   const int64_t heads = (int64_t)n_seqs * n_kv_heads, base = heads * p.n_tiles;
   const int64_t steps = ((int64_t)max_len + 63) / 64;
-  // few rows: enough workgroups to fill 256 CUs twice, each with two steps a wave at least; many
-  // rows: a workgroup a CU, of 16 steps at least
+  // A workgroup a CU at least, of 8 steps (many rows: 16) at least.  Few rows: 8 waves, two a SIMD,
+  // unless heads abound and are short: 512 heads of up to 16 steps take 27 us so and 22 with 4
+  // waves and two workgroups a CU, 600 of up to 47 73 and 77.
   const bool few = p.tile_rows != kManyTile;
-  int64_t want = ((few ? 512 : 256) + base - 1) / base, most = steps / (few ? 8 : 16);
+  p.waves = few && base > 256 && steps <= 32 ? 4 : 8;
+  int64_t want = (256 + base - 1) / base, most = steps / (few ? 8 : 16);
   if (want > most) want = most;
   if (want < 1) want = 1;
-  if (want > 256) want = 256;  // what the join takes
   p.span = (int)((steps + want - 1) / want);
-  p.wave_span = (p.span + kWaves - 1) / kWaves;
+  p.wave_span = (p.span + p.waves - 1) / p.waves;
   p.n_splits = (int)((steps + p.span - 1) / p.span);
   const int pb = block_len < 64 ? block_len : 64;
   p.n_parts = with_weights ? (max_blocks + 1) * (block_len / pb) : 0;

@@ -38,7 +38,6 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kNoMax = -1e30f;  // running maximum before the first visible key
 constexpr float kSlack = 8.f;     // the running maximum follows once it is off by 2^8
 constexpr int kScaleTop = 6;      // weights of V scales stay below 2^(kScaleTop + 1)
-constexpr int kWaves = 4;
 constexpr int kFewRows = 64;     // up to here a tile is one wave's rows
 constexpr int kManyTile = 256;   // rows of a tile beyond
 constexpr int kFewSplits = 8;    // up to here a row's splits are joined one after another
@@ -394,8 +393,8 @@ struct Rows {
   }
 };
 
-template <int D, int B, int CODE, int NT, bool WEIGHTS>
-__global__ void __launch_bounds__(64 * kWaves, 2)
+template <int D, int B, int CODE, int NT, bool WEIGHTS, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, 2)
 attn8_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __restrict__ ml,
              float* __restrict__ parts) {
   typedef Rows<D, B, NT, WEIGHTS> R;
@@ -404,8 +403,8 @@ attn8_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __restrict_
   constexpr int CHUNK = B < 64 ? B : 64;  // steps whose blocks' ids and scales a wave holds
   constexpr bool ONE = B >= 64;           // a step lies in one block
   constexpr int LDO = D + 4;
-  __shared__ __align__(16) float part_o[kWaves][16 * NT][LDO];
-  __shared__ float part_ml[kWaves][16 * NT][2];
+  __shared__ __align__(16) float part_o[WAVES][16 * NT][LDO];
+  __shared__ float part_ml[WAVES][16 * NT][2];
 
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int grp = lane >> 4, col = lane & 15;
@@ -430,7 +429,7 @@ attn8_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __restrict_
   const int steps = steps_of<B>(sq, last);
   if (split > 0 && split * plan.span >= steps) return;
   int hi = min(min(lo + plan.wave_span, (split + 1) * plan.span), steps);
-  if (split == plan.n_splits - 1 && wave == kWaves - 1) hi = steps;
+  if (split == plan.n_splits - 1 && wave == WAVES - 1) hi = steps;
 
   R r;
   r.start(a, sq, h, G, row0, grp, col);
@@ -537,7 +536,7 @@ attn8_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __restrict_
   }
 
   // The tail, a step for each of the first split's last waves (a block has at most two)
-  const int r0 = (kWaves - 1 - wave) * 64;
+  const int r0 = (WAVES - 1 - wave) * 64;
   if constexpr (WEIGHTS) r.n_parts += B / R::PB;
   if (split == 0 && r0 < B && sq.full * B + r0 < seen_by(sq, min(last, sq.n_q - 1)))
     r.tail(a, sq, z, h, G, row0, r0, lane);
@@ -556,17 +555,17 @@ attn8_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __restrict_
   constexpr int LPR = D / 4;  // lanes of a row
   const bool whole = plan.n_splits == 1;
 #pragma unroll 1
-  for (int p = threadIdx.x; p < 16 * NT * LPR; p += 64 * kWaves) {
+  for (int p = threadIdx.x; p < 16 * NT * LPR; p += 64 * WAVES) {
     const int rr = p / LPR, c = p % LPR * 4;
     const int row = row0 + rr;
     if (row >= sq.n_q * G || row >= plan.rows) continue;
     float top = part_ml[0][rr][0];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, part_ml[w][rr][0]);
+    for (int w = 1; w < WAVES; ++w) top = fmaxf(top, part_ml[w][rr][0]);
     float sum = 0.f;
     f4_t x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
       const float f = __builtin_amdgcn_exp2f(part_ml[w][rr][0] - top);
       sum += f * part_ml[w][rr][1];
       x += f * *reinterpret_cast<const f4_t*>(&part_o[w][rr][c]);
@@ -829,19 +828,28 @@ template <int D, int B, int CODE>
 void launch_kernels(const Attn8Plan& plan, const Attn8& a, float* po, float* ml, float* parts,
                     hipStream_t s) {
   const dim3 grid((unsigned)plan.n_splits, (unsigned)plan.n_tiles, (unsigned)(a.c.n_seqs * a.c.n_kv_heads));
-  const dim3 block(plan.tile_rows == kManyTile ? 512 : 64 * kWaves);
+  const dim3 block(plan.tile_rows == kManyTile ? 512 : 64 * plan.waves);
 #define KVB_ATTN(...) hipLaunchKernelGGL((__VA_ARGS__), grid, block, 0, s, a, plan, po, ml, parts)
   const bool w = a.weights_out != nullptr;
+#define KVB_FEW(NT)                                                    \
+  do {                                                                 \
+    if (plan.waves == 8) {                                             \
+      if (w) KVB_ATTN(attn8_kernel<D, B, CODE, NT, true, 8>);          \
+      else KVB_ATTN(attn8_kernel<D, B, CODE, NT, false, 8>);           \
+    } else {                                                           \
+      if (w) KVB_ATTN(attn8_kernel<D, B, CODE, NT, true, 4>);          \
+      else KVB_ATTN(attn8_kernel<D, B, CODE, NT, false, 4>);           \
+    }                                                                  \
+  } while (0)
   if (plan.tile_rows == 16) {
-    if (w) KVB_ATTN(attn8_kernel<D, B, CODE, 1, true>);
-    else KVB_ATTN(attn8_kernel<D, B, CODE, 1, false>);
+    KVB_FEW(1);
   } else if (plan.tile_rows == 32) {
-    if (w) KVB_ATTN(attn8_kernel<D, B, CODE, 2, true>);
-    else KVB_ATTN(attn8_kernel<D, B, CODE, 2, false>);
+    KVB_FEW(2);
   } else {
     if (w) KVB_ATTN(attn8_tile_kernel<D, B, CODE, true>);
     else KVB_ATTN(attn8_tile_kernel<D, B, CODE, false>);
   }
+#undef KVB_FEW
 #undef KVB_ATTN
 }
 

@@ -159,6 +159,7 @@ struct Attn8Plan {
   int n_tiles;         // tiles per (sequence, kv head)
   int n_splits;        // workgroups that share a tile's keys
   int span;            // 64-key steps of each but the last
+  int waves;           // few rows: waves of a workgroup (4 or 8)
   int wave_span;       // steps of a wave of it
   int group;           // query heads of a kv head
   int rows;            // query rows of a (sequence, kv head), at most
