@@ -713,11 +713,15 @@ hipError_t launch_cache8_evict(const Evict& a, int n_layers, hipStream_t s) {
   const int64_t rows = (int64_t)n_layers * a.n_seqs * a.n_kv_heads;
   const dim3 grid((unsigned)((rows + 3) / 4));
 #define KVB_EVICT(N) hipLaunchKernelGGL(evict_wave_kernel<N>, grid, dim3(256), 0, s, a, rows)
-  if (a.max_blocks <= 256) KVB_EVICT(4);
+  // A workgroup a row where a wave cannot hold it, and where a long row would be one wave's on an
+  // empty card (72 rows of 512 / 1024 entries: 9.7 / 17.5 us by waves, 6.8 / 7.2 so; of 256 6.1 and
+  // 6.6; 300 rows 10.1 / 18.9 and 11.7 / 12.6; 1200 rows 11.5 / 21.5 and 28.5 / 30.9).
+  if (a.max_blocks > 2048 || (a.max_blocks > 256 && rows <= 256))
+    hipLaunchKernelGGL(evict_kernel, dim3((unsigned)rows), dim3(64 * kEvictWaves), 0, s, a);
+  else if (a.max_blocks <= 256) KVB_EVICT(4);
   else if (a.max_blocks <= 512) KVB_EVICT(8);
   else if (a.max_blocks <= 1024) KVB_EVICT(16);
-  else if (a.max_blocks <= 2048) KVB_EVICT(32);
-  else hipLaunchKernelGGL(evict_kernel, dim3((unsigned)rows), dim3(64 * kEvictWaves), 0, s, a);
+  else KVB_EVICT(32);
 #undef KVB_EVICT
   return hipGetLastError();
 }
