@@ -500,7 +500,8 @@ typedef enum { KVB_PAIR_HALF = 0, KVB_PAIR_INTERLEAVED = 1 } kvb_pairing;
  * for the pairs (a, b) of the first rot_dim channels, with (c, s) row pos[t] of
  * the tables (f32 [table_len][rot_dim/2]); the other channels are y.  Arithmetic
  * is float, rounded once to dtype (KVB_BF16 or KVB_F32, of inputs and outputs
- * alike).  A token whose position lies outside [0, table_len) is written as NaN.
+ * alike); squares are summed in float, so values of a normed head are below 1e18.
+ * A token whose position lies outside [0, table_len) is written as NaN.
  * Element (t, h, c) of each tensor lies at t * token_stride + h * head_stride +
  * c, strides in elements, multiples of 8: the input may be one projection's
  * output with queries, keys and values side by side, k_out a layer of the cache.
@@ -540,9 +541,9 @@ kvb_status kvb_qk_norm_rope(int64_t n_tokens, int32_t n_q_heads, int32_t n_kv_he
  *   k_scale/v_scale f32  [n_blocks]
  *   k_tail          bf16 [L][n_seqs][Hkv][B][d]
  *   v_tail          bf16 [L][n_seqs][Hkv][d][B]         (channel-major)
- * max_blocks * B is at most 2^30.  An entry is needed once its block is full.  An entry outside [0, n_blocks)
- * is no block: its tokens are neither written nor read, nor seen by the
- * attention.  lens[b] is at most max_blocks * B + B - 1 (tokens past that are
+ * max_blocks * B is at most 2^30.  An entry is needed once its block is full.
+ * An entry outside [0, n_blocks) is no block: its tokens are neither written nor
+ * read, nor seen by the attention.  lens[b] is at most max_blocks * B + B - 1 (tokens past that are
  * neither written, read nor seen) and a negative one counts as 0. */
 typedef enum { KVB_I8 = 0, KVB_E4M3 = 1 } kvb_code;
 typedef struct {
@@ -607,8 +608,10 @@ size_t kvb_cache8_attn_workspace_bytes(const kvb_cache8_layout* layout, int32_t 
  * block's tokens of exp(softmax_scale * q . k - lse); the tokens of the tails
  * count for entry floor(lens[b] / B) where there is one.
  * Scores are 16-bit products summed in float (codes are exact in fp16; a query
- * is scaled to fp16 by a power of two), softmax, weights and sums in float; the
- * probabilities enter the product with V as fp16, those of the tails as the sum of two bfloat16.
+ * is scaled to fp16 by a power of two, which is exact but for values below 2^-14
+ * of its largest), softmax, weights and sums in float; the probabilities enter
+ * the product with V as fp16, those of the tails as the sum of two bfloat16.
+ * softmax_scale is any finite number.
  * max_queries bounds n_q, max_len bounds lens (they size the grid; results
  * do not depend on max_len but for the order of the sums).  Deterministic.
  * workspace: at least kvb_cache8_attn_workspace_bytes; calls that share it must be ordered.

@@ -595,23 +595,20 @@ kvb_status kvb_rope_scaled_table(double theta, int32_t rot_dim, const kvb_rope_s
     i0 = fmax(floor(half * log(sc.original_len / (two_pi * sc.high)) / log(theta)), 0.0);
     i1 = fmin(ceil(half * log(sc.original_len / (two_pi * sc.low)) / log(theta)), rot_dim - 1.0);
   }
-  std::vector<double> w(half);
   for (int i = 0; i < half; ++i) {
-    w[i] = pow(theta, -(2.0 * i) / rot_dim);
+    double w = pow(theta, -(2.0 * i) / rot_dim);
     if (sc.kind == KVB_ROPE_LINEAR) {
-      w[i] /= sc.factor;
+      w /= sc.factor;
     } else if (sc.kind == KVB_ROPE_PARTS) {
-      const double r = sc.original_len * w[i] / two_pi;
+      const double r = sc.original_len * w / two_pi;
       const double g = fmin(fmax((r - sc.low) / (sc.high - sc.low), 0.0), 1.0);
-      w[i] = g * w[i] + (1.0 - g) * w[i] / sc.factor;
+      w = g * w + (1.0 - g) * w / sc.factor;
     } else if (sc.kind == KVB_ROPE_INDEX) {
       const double h = fmin(fmax((i - i0) / fmax(i1 - i0, 0.001), 0.0), 1.0);
-      w[i] = (1.0 - h) * w[i] + h * w[i] / sc.factor;
+      w = (1.0 - h) * w + h * w / sc.factor;
     }
-  }
-  for (int32_t k = 0; k < n; ++k) {
-    for (int i = 0; i < half; ++i) {
-      const double a = (double)pos[k] * w[i];
+    for (int32_t k = 0; k < n; ++k) {
+      const double a = (double)pos[k] * w;
       cos_out[(size_t)k * half + i] = (float)(cos(a) * sc.attn_factor);
       sin_out[(size_t)k * half + i] = (float)(sin(a) * sc.attn_factor);
     }
