@@ -5,6 +5,11 @@
 namespace kvb {
 namespace {
 
+constexpr int kCus = 256;
+// tiles stay small up to this many rows, and up to this many rows x keys of a call
+constexpr int kFewRows = 128;
+constexpr int64_t kFewWork = 1 << 25;
+
 // splits of a row's tile that hold keys
 template <int B>
 __device__ __forceinline__ int splits_of(const Seq& sq, const Attn8Plan& plan, int row) {
@@ -133,10 +138,15 @@ __global__ void __launch_bounds__(256) attn8_finish_kernel(Attn8 a, Attn8Plan pl
   else add_weights<B>(a, plan, blockIdx.y, wg - plan.join_wgs, ml, parts);
 }
 
+// Whether a row's splits are joined one after another: up to 4, and up to 8 of many rows, where a
+// workgroup a row costs more (8 splits of 8 rows x 32 heads: 19.5 us so and 18.1 with a workgroup a
+// row; of 800 rows 46.1 and 44.7, 1600 47.3 and 47.8, 8192 x 2 159 and 165).
+bool few_splits(const Attn8Plan& plan) { return plan.n_splits <= (plan.rows > 1024 ? 8 : 4); }
+
 template <int D, int B>
 void finish(const Attn8Plan& plan, const Attn8& a, dim3 grid, const float* po, const float* ml,
             const float* parts, hipStream_t s) {
-  if (plan.n_splits > kFewSplits)
+  if (!few_splits(plan))
     hipLaunchKernelGGL((attn8_finish_kernel<D, B, true>), grid, dim3(256), 0, s, a, plan, po, ml, parts);
   else
     hipLaunchKernelGGL((attn8_finish_kernel<D, B, false>), grid, dim3(256), 0, s, a, plan, po, ml, parts);
@@ -151,6 +161,7 @@ void finish(const Attn8Plan& plan, const Attn8& a, int block_len, dim3 grid, con
   else finish<D, 128>(plan, a, grid, po, ml, parts, s);
 }
 
+
 }  // namespace
 
 Attn8Plan attn8_plan(int n_kv_heads, int head_dim, int block_len, int max_blocks, int n_q_heads,
@@ -158,25 +169,46 @@ Attn8Plan attn8_plan(int n_kv_heads, int head_dim, int block_len, int max_blocks
   Attn8Plan p{};
   p.group = n_q_heads / n_kv_heads;
   p.rows = max_queries * p.group;
-  p.tile_rows = p.rows <= 16 ? 16 : p.rows <= kFewRows ? 32 : kManyTile;
+  // Tiles of 256 rows pay once there are more than 128 rows and work for the whole card (2 heads of 8:
+  // 72 / 128 rows over 262K keys 79 us in tiles of 32 and 103 / 101 in one of 256, 160 rows 126 and
+  // 101; 400 rows over 1000 keys 13 and 38, 4000 x 4000 43 and 58, 3200 x 16000 70 and 66).
+  const int64_t heads = (int64_t)n_seqs * n_kv_heads;
+  const bool few = p.rows <= kFewRows || heads * p.rows <= kFewWork / max_len;
+  p.tile_rows = !few ? kManyTile : p.rows <= 16 ? 16 : 32;
   p.n_tiles = (p.rows + p.tile_rows - 1) / p.tile_rows;
-  const int64_t heads = (int64_t)n_seqs * n_kv_heads, base = heads * p.n_tiles;
+  const int64_t base = heads * p.n_tiles;
   const int64_t steps = ((int64_t)max_len + 63) / 64;
-  // A workgroup a CU at least, of 8 steps (many rows: 16) at least.  Few rows: 8 waves, two a SIMD,
-  // unless heads abound and are short: 512 heads of up to 16 steps take 27 us so and 22 with 4
-  // waves and two workgroups a CU, 600 of up to 47 73 and 77.
-  const bool few = p.tile_rows != kManyTile;
-  p.waves = few && base > 256 && steps <= 32 ? 4 : 8;
-  int64_t want = (256 + base - 1) / base, most = steps / (few ? 8 : 16);
-  if (want > most) want = most;
-  if (want < 1) want = 1;
+  // A CU holds one workgroup of 8 waves, two a SIMD.  Of few rows it takes 4 where heads abound and
+  // are short: 512 heads of up to 16 steps take 27 us with 8 and 22 with 4, 600 of up to 47 73 and 77.
+  p.waves = few && base > kCus && steps <= 32 ? 4 : 8;
+  int64_t want = 1;
+  if (few) {
+    // As many splits as fit on the card together, of 8 steps at least: HBM-bound, so a part of the CUs
+    // keeps the rate up, but workgroups of a second round are late (8192 tokens of 96 heads: 52 us
+    // with 2 splits, 59 with 3; of 200 heads: 90 with one, 101 with 2).
+    want = kCus / base;
+    if (want > steps / 8) want = steps / 8;
+    if (want < 1) want = 1;
+  } else {
+    // Bound by the CUs: a call takes rounds * (steps of a split + 10 for what a workgroup does beside
+    // them); the splits that fill 1 to 8 rounds are compared.
+    int64_t least = INT64_MAX;
+    for (int rounds = 1; rounds <= 8; ++rounds) {
+      int64_t n = kCus * rounds / base;
+      if (n > steps / 2) n = steps / 2;
+      if (n > kCus) n = kCus;
+      if (n < 1) n = 1;
+      const int64_t cost = (base * n + kCus - 1) / kCus * ((steps + n - 1) / n + 10);
+      if (cost < least) least = cost, want = n;
+    }
+  }
   p.span = (int)((steps + want - 1) / want);
   p.wave_span = (p.span + p.waves - 1) / p.waves;
   p.n_splits = (int)((steps + p.span - 1) / p.span);
   const int pb = block_len < 64 ? block_len : 64;
   p.n_parts = with_weights ? (max_blocks + 1) * (block_len / pb) : 0;
   const int per = 256 / (head_dim / 4);
-  if (p.n_splits > 1) p.join_wgs = p.n_splits > kFewSplits ? p.rows : (p.rows + per - 1) / per;
+  if (p.n_splits > 1) p.join_wgs = few_splits(p) ? (p.rows + per - 1) / per : p.rows;
   if (with_weights) p.weight_wgs = (max_blocks + 15) / 16;
   const auto up = [](size_t n) { return (n + 255) / 256 * 256; };
   const size_t records = (size_t)heads * p.n_splits * p.rows;

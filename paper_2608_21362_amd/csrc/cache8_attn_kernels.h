@@ -17,7 +17,7 @@
 // Few rows (attn8_kernel): HBM-bound; the waves of a workgroup take runs of steps of their
 // own, operands straight from global memory, and meet in LDS at the end; where a call has
 // few tiles, several workgroups share a tile's keys and a second launch joins them.
-// Many rows (attn8_tile_kernel): bound by the matrix cores and what feeds them; four waves of
+// Many rows (attn8_tile_kernel): bound by the matrix cores and what feeds them; eight waves of
 // 32 rows share each step's keys and values, widened to fp16 once into LDS.
 #pragma once
 #include <math.h>
@@ -38,9 +38,7 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kNoMax = -1e30f;  // running maximum before the first visible key
 constexpr float kSlack = 8.f;     // the running maximum follows once it is off by 2^8
 constexpr int kScaleTop = 6;      // weights of V scales stay below 2^(kScaleTop + 1)
-constexpr int kFewRows = 64;     // up to here a tile is one wave's rows
-constexpr int kManyTile = 256;   // rows of a tile beyond
-constexpr int kFewSplits = 8;    // up to here a row's splits are joined one after another
+constexpr int kManyTile = 256;  // rows of a tile of the many-rows kernel
 
 // four codes -> four fp16 numbers
 template <int CODE>
@@ -599,9 +597,6 @@ struct Chunk {
   __device__ __forceinline__ int lane_of_group(int st, int g) const {
     return ONE ? st / (B / 64) - blk0 : st * (64 / B) + g / (B / 16) - blk0;
   }
-  __device__ __forceinline__ int id_of_group(int st, int g) const {
-    return ONE ? __builtin_amdgcn_readlane(id, st / (B / 64) - blk0) : __shfl(id, lane_of_group(st, g), 64);
-  }
 };
 
 // Many rows: a workgroup takes 256 rows, 32 a wave, two waves a SIMD.  Each step's codes are read
@@ -613,9 +608,11 @@ struct Chunk {
 // matrix products, M(i) = the product of step i - 1's probabilities with V, then the scores of step
 // i, and a run of vector work, S(i) = the probabilities of step i, codes of K (step i + 2) and of V
 // (i + 1) widened into LDS, loads of the next ones; waves 4 to 7 are one run behind waves 0 to 3,
-// and a barrier ends every run.  (With every wave free to run, 4 waves a workgroup and 2
-// workgroups a CU, both kinds of work took turns by chance: 887 TFLOP/s.)  Three slots: a slot is
-// written two runs before it is read and two runs after it was.
+// and a barrier ends every run.  Three slots: a slot is written two runs before it is read and two
+// runs after it was.  2048 queries of 16 heads, 32K tokens of 2 (533 GFLOP): 522 us, 1020
+// TFLOP/s; with 4 waves a workgroup, 2 workgroups a CU and every wave free to run, both kinds of
+// work took turns by chance: 601 us.  Either kind alone takes 330 to 350 us; what is left is the
+// LDS, which the operands of one group and the widened codes of the other share.
 template <int D, int B, int CODE, bool WEIGHTS>
 __global__ void __launch_bounds__(512, 2)
 attn8_tile_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __restrict__ ml,

@@ -85,12 +85,17 @@ def attend(kvb, c, dev, q, nq, weights_in=None, weights=False, max_len=None, max
     return out, lse, wo
 
 
-def check_attention(c, q, nq, out, lse, weights=None, weights_in=None, scale=None):
+def check_attention(c, q, nq, out, lse, weights=None, weights_in=None, scale=None, sharp=False):
     """Against the oracle.  Bounds (u = 2^-24): a score is off by at most e = u (d + 8) sum |q k| scale, the
     product in float, and 2^-25 of the row's largest query value for each of d small query values held in fp16;
     its probability by 2 e + 2^-20 of itself, with the sums; the probability's rounding to fp16 2^-11; bfloat16
-    output 2^-8."""
+    output 2^-8.
+    sharp: scores are so far apart that probabilities leave fp16's range.  A wave holds p 2^(5 .. 6) of its largest
+    scale of V (S), and p S' / S as much of a block with scale S'; below 2^-14 such a number is off by up to 2^-25.
+    It multiplies a code c in units of at most 2^-5 S, so a key adds at most 2^-30 |c| S, where |c| S is at most
+    max |v| (int8: 127 S is the block's largest value) or 2 max |v| (e4m3: 448 S is less than twice that)."""
     scale = c.d ** -0.5 if scale is None else scale
+    size = abs(scale)
     q = q.float().cpu().numpy().astype(np.float64)
     out, lse = out.float().cpu().numpy(), None if lse is None else lse.cpu().numpy()
     G = q.shape[1] // c.H
@@ -107,9 +112,11 @@ def check_attention(c, q, nq, out, lse, weights=None, weights_in=None, scale=Non
             qa, ka = np.abs(q[rows, hq]), np.abs(k)
             off = np.zeros(nq[b])
             if len(k) and nq[b]:
-                off = 2.0 ** -24 * (c.d + 8) * scale * (qa @ ka.T).max(1)
-                off = off + 2.0 ** -25 * scale * qa.max(1) * ka.sum(1).max()
+                off = 2.0 ** -24 * (c.d + 8) * size * (qa @ ka.T).max(1)
+                off = off + 2.0 ** -25 * size * qa.max(1) * ka.sum(1).max()
             near = p @ np.abs(v) * (2.0 ** -11 + 2 * off + 2.0 ** -20)[:, None] + 2.0 ** -8 * np.abs(o) + 1e-30
+            if sharp and len(k):
+                near = near + 2.0 ** -29 * len(k) * np.abs(v).max()
             got = out[rows, hq]
             assert np.all(np.abs(got - o) <= near), (b, hq, float(np.max(np.abs(got - o) / near)))
             if lse is not None:
