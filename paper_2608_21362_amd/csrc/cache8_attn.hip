@@ -183,12 +183,14 @@ Attn8Plan attn8_plan(int n_kv_heads, int head_dim, int block_len, int max_blocks
   p.waves = few && base > kCus && steps <= 32 ? 4 : 8;
   int64_t want = 1;
   if (few) {
-    // As many splits as fit on the card together, of 8 steps at least: HBM-bound, so a part of the CUs
-    // keeps the rate up, but workgroups of a second round are late (8192 tokens of 96 heads: 52 us
-    // with 2 splits, 59 with 3; of 200 heads: 90 with one, 101 with 2).
+    // As many splits as fit on the card together: HBM-bound, so a part of the CUs keeps the rate up, but
+    // workgroups of a second round are late (8192 tokens of 96 heads: 52 us with 2 splits, 59 with 3;
+    // of 200 heads: 90 with one, 101 with 2).  Of 4 steps at least (2000 tokens: 12.1 us, of 8 steps
+    // 13.7, of 16 15.8), and no split of up to 16 steps where that saves the second launch (500 tokens:
+    // 8.5 us and 11.7, 1000: 11.6 and 12.0).
     want = kCus / base;
-    if (want > steps / 8) want = steps / 8;
-    if (want < 1) want = 1;
+    if (want > steps / 4) want = steps / 4;
+    if (want < 1 || (steps <= 16 && !with_weights)) want = 1;
   } else {
     // Bound by the CUs: a call takes rounds * (steps of a split + 10 for what a workgroup does beside
     // them); the splits that fill 1 to 8 rounds are compared.
