@@ -611,8 +611,7 @@ struct Chunk {
 // and a barrier ends every run.  Three slots: a slot is written two runs before it is read and two
 // runs after it was.  2048 queries of 16 heads, 32K tokens of 2 (533 GFLOP): 522 us, 1020
 // TFLOP/s; with 4 waves a workgroup, 2 workgroups a CU and every wave free to run, both kinds of
-// work took turns by chance: 601 us.  Either kind alone takes 330 to 350 us; what is left is the
-// LDS, which the operands of one group and the widened codes of the other share.
+// work took turns by chance: 601 us.  Either kind alone takes 330 to 350 us.
 template <int D, int B, int CODE, bool WEIGHTS>
 __global__ void __launch_bounds__(512, 2)
 attn8_tile_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __restrict__ ml,
