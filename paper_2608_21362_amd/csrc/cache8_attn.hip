@@ -77,23 +77,28 @@ __device__ __forceinline__ void join(const Attn8& a, const Attn8Plan& plan, int 
   write_row(a, sq.q0 + i, h * plan.group + row - i * plan.group, D, c * 4, x, top, sum);
 }
 
-// Accumulated weights: 16 lanes a block, each over every 16th row; the rows' log2 sums come
-// through LDS, 256 rows at a time.
+__device__ __forceinline__ void put_weight(const Attn8& a, int z, int blk, float sum) {
+  const int64_t at = (int64_t)z * a.c.max_blocks + blk;
+  a.weights_out[at] = (a.weights_in ? a.weights_in[at] : 0.f) + sum;
+}
+
+// Accumulated weights: plan.weight_lanes lanes a block (16 or 64), over the rows in turn; the rows'
+// log2 sums come through LDS, 256 rows at a time.
 template <int B>
 __device__ __forceinline__ void add_weights(const Attn8& a, const Attn8Plan& plan, int z, int wg,
                                             const float* __restrict__ ml, const float* __restrict__ parts) {
   constexpr int PB = B < 64 ? B : 64, PER = B / PB;
   __shared__ float total[256];  // log2 of a row's sum
   const int b = z / a.c.n_kv_heads;
-  const int M = a.c.max_blocks;
+  const int M = a.c.max_blocks, lanes = plan.weight_lanes, tid = threadIdx.x;
   const Seq sq = seq_of<B>(a, b);
-  const int blk = wg * 16 + threadIdx.x / 16;
+  const int blk = wg * (256 / lanes) + tid / lanes;
   const int rows = min(sq.n_q * plan.group, plan.rows);
   float sum = 0.f;
   for (int r0 = 0; r0 < rows; r0 += 256) {
+    const int r1 = min(rows, r0 + 256), r = r0 + tid;
     __syncthreads();
-    const int r = r0 + threadIdx.x;
-    if (r < rows) {
+    if (r < r1) {
       const int n = splits_of<B>(sq, plan, r);
       const int64_t rec = (int64_t)z * plan.n_splits * plan.rows + r;
       float top = kNoMax, t = 0.f;
@@ -104,10 +109,10 @@ __device__ __forceinline__ void add_weights(const Attn8& a, const Attn8Plan& pla
         const int64_t at = 2 * (rec + (int64_t)s * plan.rows);
         t += __builtin_amdgcn_exp2f(ml[at] - top) * ml[at + 1];
       }
-      total[threadIdx.x] = t == 0.f ? INFINITY : top + log2f(t);  // nothing seen: no share
+      total[tid] = t == 0.f ? INFINITY : top + log2f(t);  // nothing seen: no share
     }
     __syncthreads();
-    for (int x = r0 + threadIdx.x % 16; x < min(rows, r0 + 256); x += 16) {
+    for (int x = r0 + tid % lanes; x < r1; x += lanes) {
       const int see = seen_by(sq, (int)((unsigned)x / (unsigned)plan.group));
 #pragma unroll
       for (int p = 0; p < PER; ++p) {
@@ -118,12 +123,58 @@ __device__ __forceinline__ void add_weights(const Attn8& a, const Attn8Plan& pla
       }
     }
   }
+  for (int k = lanes / 2; k > 0; k >>= 1) sum += __shfl_xor(sum, k, 64);
+  if (blk < M && tid % lanes == 0) put_weight(a, z, blk, sum);
+}
+
+// The same with a workgroup a block (plan.weight_lanes 256): a thread takes four rows at a time, from
+// the first one that sees the block.
+template <int B>
+__device__ __forceinline__ void add_weights_of_many(const Attn8& a, const Attn8Plan& plan, int z, int blk,
+                                                    const float* __restrict__ ml,
+                                                    const float* __restrict__ parts) {
+  constexpr int PB = B < 64 ? B : 64, PER = B / PB, U = 4;
+  __shared__ float wave_sum[4];
+  const Seq sq = seq_of<B>(a, z / a.c.n_kv_heads);
+  const int rows = min(sq.n_q * plan.group, plan.rows), tid = threadIdx.x;
+  const int64_t from = (int64_t)max(0, blk * B - (sq.len - sq.n_q)) * plan.group;
+  const float2* records = reinterpret_cast<const float2*>(ml) + (int64_t)z * plan.n_splits * plan.rows;
+  const float* part = parts + ((int64_t)z * plan.n_parts + blk * PER) * plan.rows;
+  float sum = 0.f;
+  for (int64_t x0 = from + tid; x0 < rows; x0 += 256 * U) {
+    int x[U], n = 0;
+    float top[U], t[U], w[U][PER];
 #pragma unroll
-  for (int k = 8; k > 0; k >>= 1) sum += __shfl_xor(sum, k, 64);
-  if (blk < M && threadIdx.x % 16 == 0) {
-    const int64_t at = (int64_t)z * M + blk;
-    a.weights_out[at] = (a.weights_in ? a.weights_in[at] : 0.f) + sum;
+    for (int j = 0; j < U; ++j) {
+      x[j] = min((int)x0 + 256 * j, rows - 1);  // past the last one: it again, for nothing
+      const int see = (int)x0 + 256 * j < rows ? seen_by(sq, (int)((unsigned)x[j] / (unsigned)plan.group)) : 0;
+#pragma unroll
+      for (int p = 0; p < PER; ++p)
+        w[j][p] = (blk * PER + p) * PB < see ? part[(int64_t)p * plan.rows + x[j]] : -INFINITY;
+      n = max(n, splits_of<B>(sq, plan, x[j]));
+      top[j] = kNoMax, t[j] = 0.f;
+    }
+    for (int s = 0; s < n; ++s) {
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        if (s >= splits_of<B>(sq, plan, x[j])) continue;
+        const float2 y = records[(int64_t)s * plan.rows + x[j]];
+        const float next = fmaxf(top[j], y.x);
+        t[j] = t[j] * __builtin_amdgcn_exp2f(top[j] - next) + y.y * __builtin_amdgcn_exp2f(y.x - next);
+        top[j] = next;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      const float total = t[j] == 0.f ? INFINITY : top[j] + log2f(t[j]);  // nothing seen: no share
+#pragma unroll
+      for (int p = 0; p < PER; ++p) sum += __builtin_amdgcn_exp2f(w[j][p] - total);
+    }
   }
+  for (int k = 32; k > 0; k >>= 1) sum += __shfl_xor(sum, k, 64);
+  if ((tid & 63) == 0) wave_sum[tid >> 6] = sum;
+  __syncthreads();
+  if (tid == 0) put_weight(a, z, blk, wave_sum[0] + wave_sum[1] + wave_sum[2] + wave_sum[3]);
 }
 
 // What follows the attention kernel, in one launch: the first join_wgs workgroups of a (sequence, kv
@@ -135,6 +186,7 @@ __global__ void __launch_bounds__(256) attn8_finish_kernel(Attn8 a, Attn8Plan pl
                                                            const float* __restrict__ parts) {
   const int wg = blockIdx.x;
   if (wg < plan.join_wgs) join<D, B, MANY>(a, plan, blockIdx.y, wg, po, ml);
+  else if (plan.weight_lanes == 256) add_weights_of_many<B>(a, plan, blockIdx.y, wg - plan.join_wgs, ml, parts);
   else add_weights<B>(a, plan, blockIdx.y, wg - plan.join_wgs, ml, parts);
 }
 
@@ -211,7 +263,11 @@ Attn8Plan attn8_plan(int n_kv_heads, int head_dim, int block_len, int max_blocks
   p.n_parts = with_weights ? (max_blocks + 1) * (block_len / pb) : 0;
   const int per = 256 / (head_dim / 4);
   if (p.n_splits > 1) p.join_wgs = few_splits(p) ? (p.rows + per - 1) / per : p.rows;
-  if (with_weights) p.weight_wgs = (max_blocks + 15) / 16;
+  // Lanes of a block: more rows, more lanes (16 / 64 / 256: 8 rows x 128 heads 21 / 27 / 43 us, 128 rows x
+  // 4 heads 40 / 37 / 44, 512 87 / 74 / 86, 64000 rows over 8192 keys 2727 / 1349 / 621).
+  p.weight_lanes = p.rows <= 64 ? 16 : p.rows <= 1024 ? 64 : 256;
+  const int per_wg = 256 / p.weight_lanes;
+  if (with_weights) p.weight_wgs = (max_blocks + per_wg - 1) / per_wg;
   const auto up = [](size_t n) { return (n + 255) / 256 * 256; };
   const size_t records = (size_t)heads * p.n_splits * p.rows;
   p.ml_offset = p.n_splits > 1 ? up(records * head_dim * 4) : 0;

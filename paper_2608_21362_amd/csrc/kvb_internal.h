@@ -155,7 +155,7 @@ hipError_t launch_cache8_evict(const Evict& a, int n_layers, hipStream_t s);
 
 // How a kvb_cache8_attn call is cut into workgroups, and its workspace.
 struct Attn8Plan {
-  int tile_rows;       // rows of a tile: 16 or 32 (few rows), 128 (many)
+  int tile_rows;       // rows of a tile: 16 or 32 (few rows), 256 (many)
   int n_tiles;         // tiles per (sequence, kv head)
   int n_splits;        // workgroups that share a tile's keys
   int span;            // 64-key steps of each but the last
@@ -165,6 +165,7 @@ struct Attn8Plan {
   int rows;            // query rows of a (sequence, kv head), at most
   int join_wgs;        // workgroups of a (sequence, kv head) that join rows, and
   int weight_wgs;      // that add weights, in the launch that follows
+  int weight_lanes;    // lanes of a block there
   int n_parts;         // parts of up to 64 tokens of a block with a weight of their own
   size_t ml_offset;    // (max, sum) of each (sequence, kv head, split, row)
   size_t parts_offset; // log2 weight of each (sequence, kv head, part, row)

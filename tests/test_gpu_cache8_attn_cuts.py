@@ -62,6 +62,13 @@ def test_tiles_of_256_rows_over_longer_sequences_than_claimed():
     _run([9000], [700], 8, 1, 64, 64, od.I8, [6000], seed=3)
 
 
+@pytest.mark.parametrize("B,code", [(16, od.I8), (32, od.E4M3), (64, od.E4M3), (128, od.I8)])
+@pytest.mark.parametrize("claim", [1200, 4000, 40000])
+def test_weights_of_thousands_of_rows(B, code, claim):
+    """8800 rows and 200: tiles of 32 and of 256 rows, one split, 7 and many."""
+    _run([1200, 25], [1100, 25], 8, 1, 64, B, code, [claim], seed=12)
+
+
 @pytest.mark.parametrize("B,code", [(16, od.I8), (32, od.E4M3), (128, od.I8)])
 def test_four_waves(B, code):
     """More than 256 heads of up to 2048 tokens."""
