@@ -34,6 +34,11 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf8_t;
 typedef __attribute__((ext_vector_type(4))) float f4_t;
 typedef __attribute__((ext_vector_type(2))) float f2_t;
 
+template <bool V>
+struct Flag {
+  static constexpr bool value = V;
+};
+
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kNoMax = -1e30f;  // running maximum before the first visible key
 constexpr float kSlack = 8.f;     // the running maximum follows once it is off by 2^8
@@ -119,6 +124,19 @@ __device__ __forceinline__ float max64(float x) {
 #pragma unroll
   for (int k = 1; k < 16; k <<= 1) x = fmaxf(x, __shfl_xor(x, k, 64));
   return max4groups(x);
+}
+
+// What a workgroup takes: a split of the keys of a (sequence, kv head) z, and a tile of its rows.
+// Workgroups go to the 8 XCDs in turn; with plan.apart, tiles that read the same keys are kXcds apart,
+// so that they run side by side on one XCD and share its L2.
+constexpr int kXcds = 8;
+struct Place {
+  int z, split, tile;  // z < 0: none
+};
+__device__ __forceinline__ Place place(const Attn8& a, const Attn8Plan& plan) {
+  if (!plan.apart) return {(int)blockIdx.z, (int)blockIdx.x, (int)blockIdx.y};
+  const int group = blockIdx.y * kXcds + blockIdx.x % kXcds, z = group / plan.n_splits;
+  return {z < a.c.n_rows ? z : -1, group - z * plan.n_splits, (int)blockIdx.x / kXcds};
 }
 
 // One row's result: x / sum in bfloat16, and the log of the sum.
@@ -406,10 +424,12 @@ attn8_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __restrict_
 
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int grp = lane >> 4, col = lane & 15;
-  const int z = blockIdx.z, split = blockIdx.x;
+  const Place at = place(a, plan);
+  if (at.z < 0) return;
+  const int z = at.z, split = at.split;
   const int b = z / a.c.n_kv_heads, h = z - b * a.c.n_kv_heads;
   const int G = plan.group;
-  const int row0 = blockIdx.y * (16 * NT);
+  const int row0 = at.tile * (16 * NT);
   const int32_t* table = a.c.table + (int64_t)z * a.c.max_blocks;
 
   // The wave's steps: the split's, divided evenly; the last split takes what is left over where a
@@ -655,7 +675,7 @@ attn8_tile_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __rest
     int turn = lo + Ids::STEPS;  // the first step of the next chunk
     float ks = 0.f, lv = 0.f, iv = 1.f;
     uint64_t found = 0, nans = 0;
-    auto scales = [&]() {  // of the current chunk
+    auto scales = [&]() __attribute__((always_inline)) {  // of the current chunk
       found = ids[0].found;
       ks = a.c.k_scale[ids[0].id];
       const float vs = found >> lane & 1 ? a.c.v_scale[ids[0].id] : 0.f;
@@ -673,37 +693,37 @@ attn8_tile_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __rest
     const int p = PIECES >= 512 ? tid : tid & (PIECES - 1);
     const int key = p / (D / 16), kc = p % (D / 16) * 2, ch = p >> 2, vk = (p & 3) * 2;
     const int krow = (key & 12) * 4 + (key >> 4) * 4 + (key & 3);  // tile (key % 16) / 4, row of it
-    auto block_of = [&](int st, int group) {
+    auto block_of = [&](int st, int group) __attribute__((always_inline)) {
       const bool next = st >= turn;
       const int id = next ? ids[1].id : ids[0].id, blk0 = next ? ids[1].blk0 : ids[0].blk0;
       if constexpr (ONE) return __builtin_amdgcn_readlane(id, st / (B / 64) - blk0);
       else return __shfl(id, st * (64 / B) + group / (B / 16) - blk0, 64);
     };
-    auto load_k = [&](int st, uint4& kw) {
+    auto load_k = [&](int st, uint4& kw) __attribute__((always_inline)) {
       st = min(st, hi - 1);
       const int in = ONE ? st % (B / 64) * 64 + key : key % B;
       kw = *reinterpret_cast<const uint4*>(a.c.k_codes + (int64_t)block_of(st, key >> 4) * (B * D) + in * D + kc * 8);
     };
-    auto load_v = [&](int st, uint4& vw4) {
+    auto load_v = [&](int st, uint4& vw4) __attribute__((always_inline)) {
       st = min(st, hi - 1);
       const int in = ONE ? st % (B / 64) * 64 + vk * 8 : vk * 8 % B;
       vw4 = *reinterpret_cast<const uint4*>(a.c.v_codes + (int64_t)block_of(st, p & 3) * (B * D) + ch * B + in);
     };
     const int k0 = krow * KC + (kc ^ (krow & (KC - 1))), k1 = krow * KC + ((kc + 1) ^ (krow & (KC - 1)));
     const int v0 = ch * 8 + ((p & 3) ^ (ch >> 1 & 7)), v1 = ch * 8 + (((p & 3) + 4) ^ (ch >> 1 & 7));
-    auto store_k = [&](int slot, const uint4& kw) {
+    auto store_k = [&](int slot, const uint4& kw) __attribute__((always_inline)) {
       half8_t* to = kl[0] + slot * (64 * KC);
       to[k0] = widen8<CODE>(kw.x, kw.y);
       to[k1] = widen8<CODE>(kw.z, kw.w);
     };
-    auto store_v = [&](int st, int slot, const uint4& vw4) {
+    auto store_v = [&](int st, int slot, const uint4& vw4) __attribute__((always_inline)) {
       // no block at all in the chunk: no value of V may be a NaN
       const uint32_t some = (st >= turn ? ids[1].found : ids[0].found) ? ~0u : 0u;
       half8_t* to = vl[0] + slot * (D * 8);
       to[v0] = widen8<CODE>(vw4.x & some, vw4.y & some);
       to[v1] = widen8<CODE>(vw4.z & some, vw4.w & some);
     };
-    auto run_ends = [&]() {
+    auto run_ends = [&]() __attribute__((always_inline)) {
       __builtin_amdgcn_sched_barrier(0);
       __syncthreads();
       __builtin_amdgcn_sched_barrier(0);
@@ -718,7 +738,7 @@ attn8_tile_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __rest
     for (int j = 0; j < 2; ++j) vo[j] = col * 8 + ((4 * j + grp) ^ (col >> 1));
     // A run of matrix products: V of the slot before (not for the first), then scores of slot `at`.  The
     // operand pieces are read AHEAD of their products, in this order.
-    auto products = [&](int before, int at, bool first) {
+    auto products = [&](int before, int at, bool first) __attribute__((always_inline)) {
       constexpr int AHEAD = 6, NV = 2 * CT, ALL = NV + 4 * KS;
       half8_t x[8];
       f4_t acc[NT][4];
@@ -764,21 +784,20 @@ attn8_tile_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __rest
     load_v(lo + 2, vw4[1]);
     run_ends();
     if (wave >= 4) run_ends();
-    products(0, 0, true);
-    run_ends();
     int s0 = 0, s1 = 1, s2 = 2;  // slots of steps st, st + 1, st + 2
-    auto step = [&](int st, uint4& kw, uint4& vw4) {
+    auto step = [&](auto busy, int st, uint4& kw, uint4& vw4) __attribute__((always_inline)) {
       const int key = st * 64 + 16 * grp;
       const int gb = ids[0].lane_of_group(st, grp);
-      r.step(s, key, found >> gb & 1, lane_of<ONE>(ks, gb), lane_of<ONE>(lv, gb), lane_of<ONE>(iv, gb), pr);
-      if (__builtin_expect(nans != 0, 0)) r.spoil(nans >> gb & 1, key);
+      if constexpr (busy.value)
+        r.step(s, key, found >> gb & 1, lane_of<ONE>(ks, gb), lane_of<ONE>(lv, gb), lane_of<ONE>(iv, gb), pr);
+      if (busy.value && __builtin_expect(nans != 0, 0)) r.spoil(nans >> gb & 1, key);
       store_k(s2, kw);
       store_v(st + 1, s1, vw4);
       load_k(st + 4, kw);
       load_v(st + 3, vw4);
       run_ends();
       __builtin_amdgcn_s_setprio(1);
-      products(s0, s1, false);  // behind the last step: scores of what the slot holds, for nothing
+      if constexpr (busy.value) products(s0, s1, false);  // behind the last step: scores of what the slot holds, for nothing
       __builtin_amdgcn_s_setprio(0);
       if (st + 1 == turn) {  // the next chunk's blocks; st + 4 at most was asked of them so far
         ids[0] = ids[1];
@@ -790,11 +809,18 @@ attn8_tile_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __rest
       s0 = s1, s1 = s2, s2 = x;
       if (st + 1 < hi || wave < 4) run_ends();
     };
+    auto walk = [&](auto busy) __attribute__((always_inline)) {
+      if constexpr (busy.value) products(0, 0, true);
+      run_ends();
 #pragma unroll 1
-    for (int st = lo; st < hi; st += 2) {
-      step(st, kw[0], vw4[0]);
-      if (st + 1 < hi) step(st + 1, kw[1], vw4[1]);
-    }
+      for (int st = lo; st < hi; st += 2) {
+        step(busy, st, kw[0], vw4[0]);
+        if (st + 1 < hi) step(busy, st + 1, kw[1], vw4[1]);
+      }
+    };
+    // a wave without rows only feeds the others
+    if (wrow0 < sq.n_q * G) walk(Flag<true>{});
+    else walk(Flag<false>{});
   }
 
   if constexpr (WEIGHTS) r.n_parts += B / R::PB;
@@ -823,7 +849,9 @@ attn8_tile_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __rest
 template <int D, int B, int CODE>
 void launch_kernels(const Attn8Plan& plan, const Attn8& a, float* po, float* ml, float* parts,
                     hipStream_t s) {
-  const dim3 grid((unsigned)plan.n_splits, (unsigned)plan.n_tiles, (unsigned)(a.c.n_seqs * a.c.n_kv_heads));
+  dim3 grid((unsigned)plan.n_splits, (unsigned)plan.n_tiles, (unsigned)a.c.n_rows);
+  if (plan.apart)
+    grid = dim3((unsigned)(kXcds * plan.n_tiles), (unsigned)((plan.n_splits * a.c.n_rows + kXcds - 1) / kXcds));
   const dim3 block(plan.tile_rows == kManyTile ? 512 : 64 * plan.waves);
 #define KVB_ATTN(...) hipLaunchKernelGGL((__VA_ARGS__), grid, block, 0, s, a, plan, po, ml, parts)
   const bool w = a.weights_out != nullptr;

@@ -158,6 +158,7 @@ struct Attn8Plan {
   int tile_rows;       // rows of a tile: 16 or 32 (few rows), 256 (many)
   int n_tiles;         // tiles per (sequence, kv head)
   int n_splits;        // workgroups that share a tile's keys
+  int apart;           // few rows: tiles that share keys lie on one XCD
   int span;            // 64-key steps of each but the last
   int waves;           // few rows: waves of a workgroup (4 or 8)
   int wave_span;       // steps of a wave of it
