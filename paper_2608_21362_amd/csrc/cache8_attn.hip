@@ -6,7 +6,7 @@ namespace kvb {
 namespace {
 
 constexpr int kCus = 256;
-// tiles stay small up to this many rows, and up to this many rows x keys of a call
+// tiles stay small up to this many rows, and may up to this many rows x keys of a call
 constexpr int kFewRows = 128;
 constexpr int64_t kFewWork = 1 << 25;
 
@@ -223,9 +223,12 @@ Attn8Plan attn8_plan(int n_kv_heads, int head_dim, int block_len, int max_blocks
   p.rows = max_queries * p.group;
   // Tiles of 256 rows pay once there are more than 128 rows and work for the whole card (2 heads of 8:
   // 72 / 128 rows over 262K keys 79 us in tiles of 32 and 103 / 101 in one of 256, 160 rows 126 and
-  // 101; 400 rows over 1000 keys 13 and 38, 4000 x 4000 43 and 58, 3200 x 16000 70 and 66).
+  // 101; 400 rows over 1000 keys 13 and 38, 4000 x 4000 43 and 58, 3200 x 16000 70 and 66), or more
+  // small tiles than two rounds of workgroups (864 / 1512 of up to 430 keys 28 / 42 us and 34 / 31; with
+  // weights 432 / 864 33 / 47 and 35 / 40).
   const int64_t heads = (int64_t)n_seqs * n_kv_heads;
-  const bool few = p.rows <= kFewRows || heads * p.rows <= kFewWork / max_len;
+  const bool few = p.rows <= kFewRows || (heads * p.rows <= kFewWork / max_len &&
+                                          heads * ((p.rows + 31) / 32) <= (with_weights ? 512 : 1024));
   p.tile_rows = !few ? kManyTile : p.rows <= 16 ? 16 : 32;
   p.n_tiles = (p.rows + p.tile_rows - 1) / p.tile_rows;
   const int64_t base = heads * p.n_tiles;
