@@ -137,7 +137,8 @@ __device__ __forceinline__ void add_weights_of_many(const Attn8& a, const Attn8P
   __shared__ float wave_sum[4];
   const Seq sq = seq_of<B>(a, z / a.c.n_kv_heads);
   const int rows = min(sq.n_q * plan.group, plan.rows), tid = threadIdx.x;
-  const int64_t from = (int64_t)max(0, blk * B - (sq.len - sq.n_q)) * plan.group;
+  const int64_t before = (int64_t)blk * B - ((int64_t)sq.len - sq.n_q);  // queries that do not see it
+  const int64_t from = (before > 0 ? before : 0) * plan.group;
   const float2* records = reinterpret_cast<const float2*>(ml) + (int64_t)z * plan.n_splits * plan.rows;
   const float* part = parts + ((int64_t)z * plan.n_parts + blk * PER) * plan.rows;
   float sum = 0.f;

@@ -247,6 +247,32 @@ def test_evict(M, budget, first, recent):
                 assert np.array_equal(wo[l, b, h], rw, equal_nan=True), (l, b, h)
 
 
+@pytest.mark.parametrize("M,budget,first,recent", [
+    (257, 100, 1, 16), (512, 511, 0, 0), (513, 64, 4, 32), (1024, 1000, 2, 1), (1025, 0, 0, 0), (2047, 700, 0, 33),
+    (2048, 1, 0, 1), (2049, 300, 7, 7),
+])
+def test_evict_long_rows_of_many_heads(M, budget, first, recent):
+    """More than 256 rows: a wave a row up to 2048 entries."""
+    kvb, rng = _kvb(), np.random.default_rng(M)
+    L, n, H, B = 33, 4, 2, 16
+    table = rng.integers(-5, 1 << 20, (L, n, H, M)).astype(np.int32)
+    nb = np.array([M, M - 1, min(M, budget + 1), M // 2])
+    lens = (nb * B + np.array([0, 15, 9, 7])).astype(np.int32)
+    w = np.exp(rng.standard_normal((L, n, H, M)) * 4).astype(np.float32)
+    w[:, 1] = rng.integers(0, 3, (L, H, M))
+    w[:, 3][rng.random((L, H, M)) < 0.3] = np.nan
+    w[::2, 0, 0, ::3], w[1::2, 0, 0, ::2] = 0.0, -np.inf
+    _say(f"[evict] M {M} budget {budget} rows {L * n * H}")
+    t, ln, wo = _evict(kvb, table, lens, w, B, budget, first, recent)
+    assert np.array_equal(ln, lens - np.maximum(nb - budget, 0) * B)
+    for l in range(L):
+        for b in range(n):
+            for h in range(H):
+                rt, rw = od.evict(table[l, b, h], w[l, b, h], nb[b], budget, first, recent)
+                assert np.array_equal(t[l, b, h], rt), (l, b, h)
+                assert np.array_equal(wo[l, b, h], rw, equal_nan=True), (l, b, h)
+
+
 def test_evict_lengths_outside_the_table():
     kvb = _kvb()
     table = np.arange(8, dtype=np.int32).reshape(1, 2, 1, 4)

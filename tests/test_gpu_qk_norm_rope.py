@@ -72,6 +72,15 @@ def test_against_the_oracle(T, Hq, H, d, rot, norm, pairing, dtype):
     assert (cache[:, T:] == 5).all()
 
 
+@pytest.mark.parametrize("T,Hq,H,d,rot,norm,pairing,dtype", [
+    (17001, 5, 1, 128, 128, True, od.HALF, torch.bfloat16), (9001, 20, 4, 128, 64, True, od.INTERLEAVED, torch.float32),
+    (17003, 9, 7, 64, 32, True, od.HALF, torch.float32), (10001, 3, 5, 256, 256, True, od.INTERLEAVED, torch.bfloat16),
+    (10001, 3, 5, 200, 80, False, od.HALF, torch.bfloat16), (50001, 0, 5, 40, 40, True, od.HALF, torch.bfloat16)])
+def test_many_tokens(T, Hq, H, d, rot, norm, pairing, dtype):
+    """A wave takes several groups of heads; groups and heads that end inside one."""
+    test_against_the_oracle(T, Hq, H, d, rot, norm, pairing, dtype)
+
+
 def test_one_norm_without_the_other_and_in_place():
     kvb = _kvb()
     T, d = 50, 128
