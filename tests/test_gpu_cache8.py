@@ -199,6 +199,37 @@ def test_read_back(d, B, code, dtype):
             assert (got[:, :, T:] == 9).all()
 
 
+def test_more_rows_than_one_grid_dimension_takes():
+    """18000 rows of the table, K and V: the same new rows for every layer and head (strides 0)."""
+    kvb = _kvb()
+    L, n, H, d, B, T = 20, 300, 3, 64, 16, 17
+    rng = np.random.default_rng(0)
+    k, v = (od.bf16(rng.standard_normal((n, T, d))) for _ in range(2))
+    lay = kvb.cache8_layout(L * n * H, H, d, B, kvb.KVB_I8, 1)
+    table = torch.randperm(L * n * H, device="cuda").int().view(L, n, H, 1)
+    new = lambda *s, dtype: torch.full(s, 7, dtype=dtype, device="cuda")  # noqa: E731
+    arrays = (new(L * n * H, B, d, dtype=torch.uint8), new(L * n * H, dtype=torch.float32),
+              new(L * n * H, d, B, dtype=torch.uint8), new(L * n * H, dtype=torch.float32),
+              new(L, n, H, B, d, dtype=torch.bfloat16), new(L, n, H, d, B, dtype=torch.bfloat16))
+    kd, vd = (torch.from_numpy(x).bfloat16().cuda() for x in (k, v))
+    lens = new(n, dtype=torch.int32).fill_(T)
+    _say(f"[append] {2 * L * n * H} rows of K and V")
+    kvb.kvb_cache8_append(lay, L, n, cu([T] * n), T, kd, vd, 0, d, 0, table, lens, *arrays)
+    out = [new(L, H, n * T, d, dtype=torch.float32) for _ in range(2)]
+    kvb.kvb_cache8_read(lay, L, n, cu([T] * n), T, table, lens, *arrays, kvb.KVB_F32, *out, H * n * T * d, d, n * T * d)
+    torch.cuda.synchronize()
+    at = table[:, :, :, 0].long()
+    for x, codes, scale, got in ((k, arrays[0], arrays[1], out[0]), (v, arrays[2].transpose(1, 2), arrays[3], out[1])):
+        q = [od.quantise(x[b, :B], od.I8) for b in range(n)]
+        want = torch.from_numpy(np.stack([c for _, c in q]).view(np.uint8)).cuda()
+        assert torch.equal(codes[at], want[None, :, None].expand(L, n, H, B, d))
+        assert torch.equal(scale[at], torch.tensor([float(s) for s, _ in q], device="cuda")[None, :, None].expand(L, n, H))
+        back = np.stack([np.concatenate([od.values(c, s, od.I8).astype(np.float32), x[b, B:]]) for b, (s, c) in enumerate(q)])
+        assert torch.equal(got, torch.from_numpy(back.reshape(n * T, d)).cuda().expand(L, H, n * T, d))
+    assert torch.equal(arrays[4][:, :, :, 0], kd[None, :, None, B].expand(L, n, H, d))
+    assert (arrays[4][:, :, :, 1:] == 7).all() and (arrays[5][..., 1:] == 7).all()
+
+
 def test_read_leaves_what_it_cannot_find():
     kvb = _kvb()
     c = Cache([64, 40], 1, 64, 32, od.I8, extra=0)
