@@ -11,8 +11,10 @@
 //
 // Scales: a lane's 16 keys lie in one block (B >= 16).  The scale of K goes with the factor
 // of the scores; that of V into the exponent of the probabilities, relative to the largest
-// of the wave's chunk of blocks (2^7 at most, so that small blocks keep their bits in fp16),
-// and out of the sums again by one product a step.
+// of the wave's chunks of blocks so far (2^kScaleTop at most, so that small blocks keep their bits in
+// fp16), and out of the sums again by one product a step.  That factor is 2^-40 at least, so sums and
+// weights keep their floats' accuracy however small a block's values are; a probability of at most 2^8
+// times 2^-40 is 0 in fp16 anyway, so the product with V is the same with any smaller one.
 //
 // Few rows (attn8_kernel): HBM-bound; the waves of a workgroup take runs of steps of their
 // own, operands straight from global memory, and meet in LDS at the end; where a call has
@@ -42,7 +44,7 @@ struct Flag {
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kNoMax = -1e30f;  // running maximum before the first visible key
 constexpr float kSlack = 8.f;     // the running maximum follows once it is off by 2^8
-constexpr int kScaleTop = 6;      // weights of V scales stay below 2^(kScaleTop + 1)
+constexpr int kScaleTop = 6;      // weights of V scales stay below 2^kScaleTop
 constexpr int kManyTile = 256;  // rows of a tile of the many-rows kernel
 
 // four codes -> four fp16 numbers
@@ -223,6 +225,11 @@ struct Rows {
       if (e > vexp) unit(e);
     }
   }
+  // the weight of a scale of V: its size in the outputs' unit.  Blocks of zeros or NaN have codes 0, any
+  // weight will do; the smallest is 2^-40 (a float's reciprocal and its logarithm stay exact enough)
+  __device__ __forceinline__ float weight_of(float vs) const {
+    return vs > 0.f ? fmaxf(__builtin_ldexpf(vs, kScaleTop - vexp), 0x1p-40f) : 1.f;
+  }
   // outputs in units of 2^(e - kScaleTop) from here on
   __device__ __forceinline__ void unit(int e) {
     const float f = __builtin_ldexpf(1.f, vexp - e);
@@ -269,8 +276,8 @@ struct Rows {
     }
   }
 
-  // Scores of a step of coded keys -> the operand of the product with V.  lv, iv, nan: log2 of the
-  // scale of V in the outputs' unit, its reciprocal, and whether it is a NaN (this lane's block).
+  // Scores of a step of coded keys -> the operand of the product with V.  lv, iv: log2 of the weight of
+  // the scale of V, and the weight's reciprocal (this lane's block).
   __device__ __forceinline__ void step(float (&s)[NT][16], int key, bool have, float ks, float lv,
                                        float iv, half8_t (&pr)[NT][2]) {
     bool clear = have;
@@ -503,9 +510,7 @@ attn8_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __restrict_
     load_k(c0);
     load_v(c0);
     r.fit(max64(vs));
-    // 2^lv is the scale in the outputs' unit; a block of zeros or NaN has codes 0, any scale will do
-    const bool none = !(vs > 0.f);
-    const float vw = none ? 1.f : __builtin_ldexpf(vs, kScaleTop - r.vexp);
+    const float vw = r.weight_of(vs);
     const float lv = __builtin_amdgcn_logf(vw), iv = 1.f / vw;
     const uint64_t nans = __ballot(vs != vs);
 
@@ -680,8 +685,7 @@ attn8_tile_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __rest
       ks = a.c.k_scale[ids[0].id];
       const float vs = found >> lane & 1 ? a.c.v_scale[ids[0].id] : 0.f;
       r.fit(max64(vs));
-      // 2^lv is the scale in the outputs' unit; a block of zeros or NaN has codes 0, any scale will do
-      const float vw = vs > 0.f ? __builtin_ldexpf(vs, kScaleTop - r.vexp) : 1.f;
+      const float vw = r.weight_of(vs);
       lv = __builtin_amdgcn_logf(vw), iv = 1.f / vw;
       nans = __ballot(vs != vs);
     };

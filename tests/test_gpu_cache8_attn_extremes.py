@@ -1,0 +1,61 @@
+"""Attention over the 8-bit cache at the ends of what its inputs can hold: values of V so small or so far
+apart that their scales leave a float's normal range.  Sums of probabilities, and the weights that come of
+them, do not depend on V."""
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+from cache8_check import Cache, attend, check_attention
+from oracle import decode as od
+
+pytestmark = pytest.mark.gpu
+
+CODES = pytest.mark.parametrize("code", [od.I8, od.E4M3], ids=["i8", "e4m3"])
+# queries and max_len: the kernel of few rows (in one piece, and split), and that of tiles of 256 rows
+KINDS = pytest.mark.parametrize("nq,claim", [(1, 700), (1, 20000), (40, 2 ** 30), (40, 60000)],
+                                ids=["few", "split", "tile", "tile_split"])
+
+
+@pytest.fixture(autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+def _say(*a):
+    print("[extremes]", *a, file=sys.stderr, flush=True)
+
+
+def _normal(seed, *shape):
+    return od.bf16(np.random.default_rng(seed).standard_normal(shape))
+
+
+def _attend(c, q, nq, claim, scale=None):
+    from paper_2608_21362_amd import kvb
+
+    win = torch.rand((c.n, c.H, c.M), device="cuda")
+    out, lse, w = attend(kvb, c, c.device(), q, [nq], win, True, max_len=claim, scale=scale)
+    torch.cuda.synchronize()
+    return out, lse, w, win
+
+
+@CODES
+@KINDS
+@pytest.mark.parametrize("B,d,T", [(16, 64, 2300), (64, 128, 700)])
+@pytest.mark.parametrize("big,small", [(1.0, 2.0 ** -126), (1.0, 2.0 ** -133), (100.0, 2.0 ** -126), (100.0, 2.0 ** -128),
+                                       (1e4, 2.0 ** -120), (1e4, 2.0 ** -123), (1e4, 2.0 ** -133)])
+def test_sums_do_not_depend_on_the_size_of_the_values(big, small, B, d, T, nq, claim, code):
+    """Blocks of V at a float's lower end among ordinary ones (and 64 of them before the first ordinary one)."""
+    _say(f"V {big} and {small} B {B} d {d} queries {nq} max_len {claim} code {code}")
+    c = Cache([T], 1, d, B, code, seed=1)
+    k, v = _normal(1, T, d), od.bf16(_normal(2, T, d) * big)
+    rng = np.random.default_rng(3)
+    for j in range(T // B):
+        if j % 3 == 1 or (B == 16 and j < 64):
+            v[j * B:(j + 1) * B] = np.float32(small) * rng.integers(-2, 3, (B, d))
+    c.put(0, 0, 0, k, v)
+    q = torch.from_numpy(_normal(4, nq, 4, d)).bfloat16().cuda()
+    out, lse, w, win = _attend(c, q, nq, claim)
+    check_attention(c, q, [nq], out, lse, w, win, sharp=True)
