@@ -44,6 +44,7 @@ struct Flag {
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kNoMax = -1e30f;  // running maximum before the first visible key
 constexpr float kSlack = 8.f;     // the running maximum follows once it is off by 2^8
+constexpr float kFar = 0x1p20f;   // below it a score's rounding (2^-4 at most) is no matter to 2^score's range
 constexpr int kScaleTop = 6;      // weights of V scales stay below 2^kScaleTop
 constexpr int kManyTile = 256;  // rows of a tile of the many-rows kernel
 
@@ -164,6 +165,7 @@ struct Rows {
   float m[NT], l[NT];
   f4_t o[NT][CT];
   int vexp;
+  bool far;      // a running maximum is beyond kFar (of any row of the wave, at any time)
   float* parts;  // log2 weights of the parts, of plan.rows rows each
   int n_parts;   // the parts below this are written
   int row, rows; // this lane's first row (the others follow 16 apart), rows of a part
@@ -215,7 +217,7 @@ struct Rows {
 #pragma unroll
       for (int c = 0; c < CT; ++c) o[n][c] = (f4_t){0.f, 0.f, 0.f, 0.f};
     }
-    vexp = -127;
+    vexp = -127, far = false;
   }
 
   // room for scales of V up to `big`
@@ -243,20 +245,28 @@ struct Rows {
   // Raw scores -> probabilities times 2^lv (the scale of V) of the step: exp2(f s - m + lv).  The
   // running maximum, the sums (iv = 2^-lv takes the scale out again) and the part's weight
   // follow.  f >= 0; masked scores are -infinity with f = 1.  key: the first of this lane's 16.
+  // Beyond kFar the exact f s and the rounded maximum may be far apart, and lv lost in the maximum: there
+  // the rounded products are compared, so that no probability passes 2^kSlack.
   __device__ __forceinline__ void soften(int n, float (&s)[16], float f, float lv, float iv, int key) {
     float top = s[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
     top = max4groups(top * f);
-    if (__any(top > m[n] + kSlack)) {
-      const float next = top > m[n] + kSlack ? top : m[n];
+    if (__any(top - m[n] > kSlack)) {
+      const float next = top - m[n] > kSlack ? top : m[n];
       const float g = __builtin_amdgcn_exp2f(m[n] - next);
       l[n] *= g;
 #pragma unroll
       for (int c = 0; c < CT; ++c) o[n][c] *= g;
       m[n] = next;
+      far = far || __any(fabsf(next) > kFar && next != kNoMax);
     }
-    const float bias = lv - m[n];
+    float bias = lv - m[n];
+    if (__builtin_expect(far, 0)) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = s[i] * f - m[n];
+      f = 1.f, bias = lv;
+    }
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {

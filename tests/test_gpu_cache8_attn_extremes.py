@@ -1,6 +1,6 @@
 """Attention over the 8-bit cache at the ends of what its inputs can hold: values of V so small or so far
 apart that their scales leave a float's normal range.  Sums of probabilities, and the weights that come of
-them, do not depend on V."""
+them, do not depend on V.  And scores of any size."""
 import sys
 
 import numpy as np
@@ -59,3 +59,35 @@ def test_sums_do_not_depend_on_the_size_of_the_values(big, small, B, d, T, nq, c
     q = torch.from_numpy(_normal(4, nq, 4, d)).bfloat16().cuda()
     out, lse, w, win = _attend(c, q, nq, claim)
     check_attention(c, q, [nq], out, lse, w, win, sharp=True)
+
+
+def _one_key(c, q, nq, claim, scale, at):
+    """All of the weight is on key `at`."""
+    out, lse, w, win = _attend(c, q, nq, claim, scale)
+    check_attention(c, q, [nq], out, lse, w, win, scale=scale)
+    want = torch.from_numpy(c.v[0, 0, 0][at]).cuda()
+    # the sum's term is its own divisor but for the rounding of the probability to fp16; one rounding of the output
+    assert ((out.double() - want).abs() <= (2.0 ** -8 + 2.0 ** -10) * want.abs()).all()
+    share = (w - win).double()[0, 0]
+    rows = q.shape[0] * q.shape[1]
+    assert abs(share[at // c.B].item() - rows) <= 2.0 ** -16 * rows
+    share[at // c.B] = 0
+    assert share.abs().max() <= 2.0 ** -20
+
+
+@CODES
+@KINDS
+@pytest.mark.parametrize("at", [5, 333, 650])
+@pytest.mark.parametrize("B", [16, 64])
+@pytest.mark.parametrize("scale", [1e5, 1e7, 1e9, 1e30])
+def test_large_scores(scale, B, at, nq, claim, code):
+    """Scores whose last bit is worth more than a probability's whole range.  q . k of one key is about
+    4 |q|^2, over 350; of the others |q| times a normal number, below 80: further apart than any rounding."""
+    _say(f"scale {scale} key {at} B {B} queries {nq} max_len {claim} code {code}")
+    T, d = 700, 128
+    c = Cache([T], 1, d, B, code, seed=3)
+    k, v, u = _normal(8, T, d), _normal(9, T, d), _normal(10, d)
+    k[at] = od.bf16(u * 4)
+    c.put(0, 0, 0, k, v)
+    q = u * np.random.default_rng(11).uniform(0.9, 1.1, (nq, 16, d))  # rows whose scores round up and down
+    _one_key(c, torch.from_numpy(q).bfloat16().cuda(), nq, claim, scale, at)
