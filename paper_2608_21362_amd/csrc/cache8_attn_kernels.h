@@ -165,7 +165,7 @@ struct Rows {
   float m[NT], l[NT];
   f4_t o[NT][CT];
   int vexp;
-  bool far;      // a running maximum is beyond kFar (of any row of the wave, at any time)
+  uint64_t far;  // not 0: a running maximum is or was beyond kFar
   float* parts;  // log2 weights of the parts, of plan.rows rows each
   int n_parts;   // the parts below this are written
   int row, rows; // this lane's first row (the others follow 16 apart), rows of a part
@@ -217,7 +217,7 @@ struct Rows {
 #pragma unroll
       for (int c = 0; c < CT; ++c) o[n][c] = (f4_t){0.f, 0.f, 0.f, 0.f};
     }
-    vexp = -127, far = false;
+    vexp = -127, far = 0;
   }
 
   // room for scales of V up to `big`
@@ -252,21 +252,22 @@ struct Rows {
 #pragma unroll
     for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
     top = max4groups(top * f);
-    if (__any(top - m[n] > kSlack)) {
-      const float next = top - m[n] > kSlack ? top : m[n];
-      const float g = __builtin_amdgcn_exp2f(m[n] - next);
+    float base = m[n];
+    if (__builtin_expect((__ballot(top - base > kSlack) | far) != 0, 0)) {
+      const float next = top - base > kSlack ? top : base;
+      const float g = __builtin_amdgcn_exp2f(base - next);
       l[n] *= g;
 #pragma unroll
       for (int c = 0; c < CT; ++c) o[n][c] *= g;
-      m[n] = next;
-      far = far || __any(fabsf(next) > kFar && next != kNoMax);
-    }
-    float bias = lv - m[n];
-    if (__builtin_expect(far, 0)) {
+      m[n] = base = next;
+      far |= __ballot(fabsf(next) > kFar && next != kNoMax);
+      if (__builtin_expect(far != 0, 0)) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = s[i] * f - m[n];
-      f = 1.f, bias = lv;
+        for (int i = 0; i < 16; ++i) s[i] = s[i] * f - next;
+        f = 1.f, base = 0.f;
+      }
     }
+    const float bias = lv - base;
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
