@@ -42,7 +42,7 @@ struct Flag {
 };
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kNoMax = -1e30f;  // running maximum before the first visible key
+constexpr float kNoMax = -0x1.fffffep127f;  // running maximum before the first visible key: no score is below
 constexpr float kSlack = 8.f;     // the running maximum follows once it is off by 2^8
 constexpr float kFar = 0x1p20f;   // below it a score's rounding (2^-4 at most) is no matter to 2^score's range
 constexpr int kScaleTop = 6;      // weights of V scales stay below 2^kScaleTop

@@ -91,3 +91,19 @@ def test_large_scores(scale, B, at, nq, claim, code):
     c.put(0, 0, 0, k, v)
     q = u * np.random.default_rng(11).uniform(0.9, 1.1, (nq, 16, d))  # rows whose scores round up and down
     _one_key(c, torch.from_numpy(q).bfloat16().cuda(), nq, claim, scale, at)
+
+
+@CODES
+@KINDS
+@pytest.mark.parametrize("at", [5, 333, 650])
+def test_scores_far_below_zero(at, nq, claim, code):
+    """Every score of a row is below -1e33: the largest of them still has all of the weight."""
+    _say(f"key {at} queries {nq} max_len {claim} code {code}")
+    T, d, B = 700, 128, 64
+    c = Cache([T], 1, d, B, code, seed=4)
+    v, u = _normal(11, T, d), _normal(12, d)
+    k = od.bf16(u * np.random.default_rng(13).uniform(1, 2, (T, 1)))
+    k[at] = od.bf16(u * 0.5)
+    c.put(0, 0, 0, k, v)
+    q = torch.from_numpy(np.broadcast_to(u, (nq, 4, d)).copy()).bfloat16().cuda()
+    _one_key(c, q, nq, claim, -1e32, at)
