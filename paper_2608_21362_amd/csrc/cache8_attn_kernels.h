@@ -46,6 +46,7 @@ constexpr float kNoMax = -0x1.fffffep127f;  // running maximum before the first 
 constexpr float kSlack = 8.f;     // the running maximum follows once it is off by 2^8
 constexpr float kFar = 0x1p20f;   // below it a score's rounding (2^-4 at most) is no matter to 2^score's range
 constexpr int kScaleTop = 6;      // weights of V scales stay below 2^kScaleTop
+constexpr int kTailTop = 16;      // outputs' unit (log2) over a tail, at least
 constexpr int kManyTile = 256;  // rows of a tile of the many-rows kernel
 
 // four codes -> four fp16 numbers
@@ -142,13 +143,16 @@ __device__ __forceinline__ Place place(const Attn8& a, const Attn8Plan& plan) {
   return {z < a.c.n_rows ? z : -1, group - z * plan.n_splits, (int)blockIdx.x / kXcds};
 }
 
-// One row's result: x / sum in bfloat16, and the log of the sum.
+// Outputs are divided by their sums before they leave a wave, and joined by weights whose sum is 1, so that
+// nothing passes the largest value of V (a sum of probabilities, up to 2^8 a key, times V may leave a float).
+// A reciprocal within 2^-23 will do (a token over 2000: 11.67 us, with quotients 11.75).
+__device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum); }
+
+// One row's result x in bfloat16, and the log of its sum.
 __device__ __forceinline__ void write_row(const Attn8& a, int q, int head, int D, int c, f4_t x,
                                           float top, float sum) {
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
   const int64_t r = (int64_t)q * a.n_q_heads + head;
-  *reinterpret_cast<uint2*>(a.out + r * D + c) =
-      make_uint2(pack_bf16x2(x[0] * inv, x[1] * inv), pack_bf16x2(x[2] * inv, x[3] * inv));
+  *reinterpret_cast<uint2*>(a.out + r * D + c) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
   if (a.lse && c == 0) a.lse[r] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
 
@@ -332,7 +336,8 @@ struct Rows {
   // are cleared.
   __device__ __forceinline__ void tail(const Attn8& a, const Seq& sq, int z, int h, int G, int row0, int r0,
                                        int lane) {
-    if (vexp < kScaleTop) unit(kScaleTop);  // 1 at least: the sums fit a float if the outputs do
+    // up to 128 probabilities of up to 2^kSlack, times bfloat16 values, in a unit of 2^16 fit a float
+    if (vexp < kScaleTop + kTailTop) unit(kScaleTop + kTailTop);
     const uint16_t* kt = a.c.k_tail + (int64_t)z * B * D;
     const uint16_t* vt = a.c.v_tail + (int64_t)z * B * D;
     const int grp = lane >> 4, col = lane & 15, t0 = sq.full * B + r0;
@@ -580,10 +585,11 @@ attn8_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __restrict_
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     r.l[n] = sum4groups(r.l[n]);
+    const float inv = inverse(r.l[n]);
     if (grp == 0) part_ml[wave][n * 16 + col][0] = r.m[n], part_ml[wave][n * 16 + col][1] = r.l[n];
 #pragma unroll
     for (int c = 0; c < CT; ++c)
-      *reinterpret_cast<f4_t*>(&part_o[wave][n * 16 + col][c * 16 + grp * 4]) = r.o[n][c] * unit;
+      *reinterpret_cast<f4_t*>(&part_o[wave][n * 16 + col][c * 16 + grp * 4]) = r.o[n][c] * inv * unit;
   }
   __syncthreads();
   constexpr int LPR = D / 4;  // lanes of a row
@@ -596,14 +602,16 @@ attn8_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __restrict_
     float top = part_ml[0][rr][0];
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) top = fmaxf(top, part_ml[w][rr][0]);
-    float sum = 0.f;
-    f4_t x = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f, f[WAVES];
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
-      const float f = __builtin_amdgcn_exp2f(part_ml[w][rr][0] - top);
-      sum += f * part_ml[w][rr][1];
-      x += f * *reinterpret_cast<const f4_t*>(&part_o[w][rr][c]);
+      f[w] = __builtin_amdgcn_exp2f(part_ml[w][rr][0] - top) * part_ml[w][rr][1];
+      sum += f[w];
     }
+    const float inv = inverse(sum);
+    f4_t x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) x += f[w] * inv * *reinterpret_cast<const f4_t*>(&part_o[w][rr][c]);
     const int64_t rec = ((int64_t)z * plan.n_splits + split) * plan.rows + row;
     if ((!whole || WEIGHTS) && c == 0) ml[2 * rec] = top, ml[2 * rec + 1] = sum;
     if (!whole) {
@@ -847,7 +855,7 @@ attn8_tile_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __rest
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     const int row = wrow0 + n * 16 + col;
-    const float sum = sum4groups(r.l[n]);
+    const float sum = sum4groups(r.l[n]), inv = inverse(sum);
     if (row >= sq.n_q * G || row >= plan.rows) continue;
     const int64_t rec = ((int64_t)z * plan.n_splits + split) * plan.rows + row;
     if ((!whole || WEIGHTS) && grp == 0) ml[2 * rec] = r.m[n], ml[2 * rec + 1] = sum;
@@ -855,8 +863,9 @@ attn8_tile_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __rest
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
       const int ch = c * 16 + grp * 4;
-      if (whole) write_row(a, sq.q0 + i, h * G + row - i * G, D, ch, r.o[n][c] * unit, r.m[n], sum);
-      else *reinterpret_cast<f4_t*>(po + rec * D + ch) = r.o[n][c] * unit;
+      const f4_t x = r.o[n][c] * inv * unit;
+      if (whole) write_row(a, sq.q0 + i, h * G + row - i * G, D, ch, x, r.m[n], sum);
+      else *reinterpret_cast<f4_t*>(po + rec * D + ch) = x;
     }
   }
 }

@@ -1,6 +1,6 @@
 """Attention over the 8-bit cache at the ends of what its inputs can hold: values of V so small or so far
-apart that their scales leave a float's normal range.  Sums of probabilities, and the weights that come of
-them, do not depend on V.  And scores of any size."""
+apart that their scales leave a float's normal range, or so large that sums over them do; scores of any size.
+Sums of probabilities, and the weights that come of them, do not depend on V."""
 import sys
 
 import numpy as np
@@ -107,3 +107,21 @@ def test_scores_far_below_zero(at, nq, claim, code):
     c.put(0, 0, 0, k, v)
     q = torch.from_numpy(np.broadcast_to(u, (nq, 4, d)).copy()).bfloat16().cuda()
     _one_key(c, q, nq, claim, -1e32, at)
+
+
+@CODES
+@KINDS
+@pytest.mark.parametrize("coded,tail", [(2.0 ** 124, 2.0 ** 124), (1.0, 2.0 ** 124), (2.0 ** 124, 1.0), (2.0 ** -80, 2.0 ** 124), (2.0 ** -80, 2.0 ** -80)])
+def test_values_near_the_end_of_the_range(coded, tail, nq, claim, code):
+    """Sums of probabilities times V leave a float where their quotient does not."""
+    _say(f"V {coded} tail {tail} queries {nq} max_len {claim} code {code}")
+    T, d, B = 700, 128, 64
+    c = Cache([T], 1, d, B, code, seed=5)
+    k, v = _normal(14, T, d), _normal(15, T, d).astype(np.float64)
+    v[:T // B * B] *= coded
+    v[T // B * B:] *= tail
+    assert np.abs(v).max() < 3.3e38
+    c.put(0, 0, 0, k, od.bf16(v))
+    q = torch.from_numpy(_normal(16, nq, 4, d)).bfloat16().cuda()
+    out, lse, w, win = _attend(c, q, nq, claim)
+    check_attention(c, q, [nq], out, lse, w, win, sharp=coded != tail)
