@@ -6,6 +6,7 @@ namespace kvb {
 namespace {
 
 constexpr int kCus = 256;
+constexpr unsigned kFinishX = 1 << 22;
 // tiles stay small up to this many rows, and may up to this many rows x keys of a call
 constexpr int kFewRows = 128;
 constexpr int64_t kFewWork = 1 << 25;
@@ -190,7 +191,8 @@ __global__ void __launch_bounds__(256) attn8_finish_kernel(Attn8 a, Attn8Plan pl
                                                            const float* __restrict__ po,
                                                            const float* __restrict__ ml,
                                                            const float* __restrict__ parts) {
-  const int wg = blockIdx.x;
+  const int wg = (int)(blockIdx.z * gridDim.x + blockIdx.x);
+  if (wg >= plan.join_wgs + plan.weight_wgs) return;
   if (wg < plan.join_wgs) join<D, B, MANY>(a, plan, blockIdx.y, wg, po, ml);
   else if (plan.weight_lanes == 256) add_weights_of_many<B>(a, plan, blockIdx.y, wg - plan.join_wgs, ml, parts);
   else add_weights<B>(a, plan, blockIdx.y, wg - plan.join_wgs, ml, parts);
@@ -218,7 +220,6 @@ void finish(const Attn8Plan& plan, const Attn8& a, int block_len, dim3 grid, con
   else if (block_len == 64) finish<D, 64>(plan, a, grid, po, ml, parts, s);
   else finish<D, 128>(plan, a, grid, po, ml, parts, s);
 }
-
 
 }  // namespace
 
@@ -297,7 +298,10 @@ hipError_t launch_cache8_attn(const Attn8Plan& plan, const Attn8& a, int head_di
   kernels(plan, a, block_len, po, ml, parts, s);
   if (hipError_t e = hipGetLastError()) return e;
   if (plan.join_wgs + plan.weight_wgs == 0) return hipSuccess;
-  const dim3 grid((unsigned)(plan.join_wgs + plan.weight_wgs), (unsigned)(a.c.n_seqs * a.c.n_kv_heads));
+  // up to 2^22 workgroups in x, the others in z: a long table has more than 2^32 / 256 (work items of a
+  // grid dimension past 2^32 are lost)
+  const unsigned wgs = (unsigned)(plan.join_wgs + plan.weight_wgs), across = wgs < kFinishX ? wgs : kFinishX;
+  const dim3 grid(across, (unsigned)(a.c.n_seqs * a.c.n_kv_heads), (wgs + across - 1) / across);
   if (head_dim == 128) finish<128>(plan, a, block_len, grid, po, ml, parts, s);
   else finish<64>(plan, a, block_len, grid, po, ml, parts, s);
   return hipGetLastError();
