@@ -52,3 +52,36 @@ def test_weights_of_the_longest_table():
     assert (w[..., held:] == 1).all()
     c.M = held
     check_attention(c, q, [9], out, lse, w[..., :held], win[..., :held])
+
+
+def test_eviction_of_more_long_rows_than_one_grid_dimension_takes():
+    """2^22 rows of 2049 entries: a workgroup of 1024 threads a row.  Three sequences are over their budget."""
+    from paper_2608_21362_amd import kvb
+
+    _need(110)
+    L, n, M, B, budget = 4, 1 << 20, 2049, 16, 2000
+    table = torch.empty((L, n, M), dtype=torch.int32, device="cuda")
+    for l in range(L):  # numbers that are finite floats too: the weights are the same bits
+        torch.randint(0x3F800000, 0x41000000, (n, M), dtype=torch.int32, device="cuda", out=table[l])
+    weights = table.view(torch.float32)
+    lens = torch.zeros(n, dtype=torch.int32, device="cuda")
+    over = [0, n // 2 + 1, n - 1]
+    lens[over] = M * B + 3
+    table_out, weights_out = torch.empty_like(table), torch.empty_like(weights)
+    lens_out = torch.empty_like(lens)
+    lay = kvb.cache8_layout(1, 1, 64, B, kvb.KVB_I8, M)
+    _say("2^22 rows of 2049 entries")
+    kvb.kvb_cache8_evict(lay, L, n, budget, 1, 16, table, lens, weights, table_out, lens_out, weights_out)
+    torch.cuda.synchronize()
+    want = lens.clone()
+    want[over] -= (M - budget) * B
+    assert torch.equal(lens_out, want)
+    for l in range(L):
+        for b in over:
+            t, w = od.evict(table[l, b].cpu().numpy(), weights[l, b].cpu().numpy(), M, budget, 1, 16)
+            assert torch.equal(table_out[l, b].cpu(), torch.from_numpy(t))
+            assert torch.equal(weights_out[l, b].cpu(), torch.from_numpy(w))
+            table_out[l, b], weights_out[l, b] = table[l, b], weights[l, b]
+        for x, y in ((table_out, table), (weights_out.view(torch.int32), table)):
+            for part in range(0, n, n // 8):
+                assert torch.equal(x[l, part:part + n // 8], y[l, part:part + n // 8]), (l, part)
