@@ -508,8 +508,8 @@ typedef enum { KVB_PAIR_HALF = 0, KVB_PAIR_INTERLEAVED = 1 } kvb_pairing;
  * Outputs may be their inputs (the same address and strides).  rot_dim 0
  * (tables and pos NULL) only norms; n_q_heads or n_kv_heads may be 0 (its
  * pointers NULL).  q_weight, k_weight: f32 [head_dim].  pos: i32 [n_tokens].
- * Errors: KVB_EINVAL (incl. n_tokens * (n_q_heads + n_kv_heads) of 2^26 and
- * more), KVB_EUNSUPPORTED (head_dim not a multiple of 8 up to 256, rot_dim not a
+ * Errors: KVB_EINVAL (incl. n_tokens * (n_q_heads + n_kv_heads) above 2^26 -
+ * 4), KVB_EUNSUPPORTED (head_dim not a multiple of 8 up to 256, rot_dim not a
  * multiple of 8). */
 kvb_status kvb_qk_norm_rope(int64_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads,
                             int32_t head_dim, kvb_dtype dtype, const void* q,

@@ -633,8 +633,9 @@ kvb_status kvb_qk_norm_rope(int64_t n_tokens, int32_t n_q_heads, int32_t n_kv_he
   if (head_dim % 8 != 0 || head_dim > 256 || rot_dim % 8 != 0)
     return fail(KVB_EUNSUPPORTED, "head_dim %d, rot_dim %d: multiples of 8 up to 256", head_dim,
                 rot_dim);
-  REQUIRE(n_tokens * (n_q_heads + (int64_t)n_kv_heads) < (int64_t)1 << 26,
-          "too many heads: n_tokens * (n_q_heads + n_kv_heads) is not below 2^26");
+  // four waves a workgroup of 256, a wave a head at most: below 2^32 work items
+  REQUIRE(n_tokens * (n_q_heads + (int64_t)n_kv_heads) <= ((int64_t)1 << 26) - 4,
+          "too many heads: n_tokens * (n_q_heads + n_kv_heads) is above 2^26 - 4");
   REQUIRE(dtype == KVB_BF16 || dtype == KVB_F32, "dtype must be BF16 or F32");
   REQUIRE(pairing == KVB_PAIR_HALF || pairing == KVB_PAIR_INTERLEAVED, "unknown pairing %d",
           (int)pairing);

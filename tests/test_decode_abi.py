@@ -100,6 +100,13 @@ def test_norm_rope_rejects(over, status):
     assert _status(_norm_rope, **over) == status
 
 
+@pytest.mark.parametrize("tokens,heads", [(2 ** 26 - 3, (1, 0)), (2 ** 26 - 3, (0, 1)), (2 ** 25 - 1, (1, 1))])
+def test_norm_rope_takes_at_most_2_to_26_less_4_heads(tokens, heads):
+    assert _status(_norm_rope, n_tokens=tokens, n_q_heads=heads[0], n_kv_heads=heads[1]) == EINVAL
+    if NO_GPU:  # what fits passes every check
+        assert _status(_norm_rope, n_tokens=tokens - 1, n_q_heads=heads[0], n_kv_heads=heads[1]) == kvb.KVB_EHIP
+
+
 # ---- the 8-bit cache --------------------------------------------------------------
 
 def _layout(**over):
