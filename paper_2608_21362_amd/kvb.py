@@ -133,14 +133,19 @@ def _check(status: int):
 
 
 def _p(t):
-    """Device (or host) address of a torch tensor / numpy array, 0 for None.  Tensors first: a
-    call has up to ten of them and a few microseconds on the host."""
+    """Device (or host) address of a torch tensor / numpy array, 0 for None, an address as it is;
+    AttributeError for anything else (ctypes would take the address of a string's bytes).
+    Tensors first: a call has up to ten of them and a few microseconds on the host."""
     if t is None or type(t) is int:
         return t
     try:
         return t.data_ptr()
     except AttributeError:
-        return t.ctypes.data if isinstance(t, np.ndarray) else t
+        if isinstance(t, np.ndarray):
+            return t.ctypes.data
+        if isinstance(t, int):
+            return t
+        raise
 
 
 _torch = None  # imported with the first call that needs the current stream

@@ -198,6 +198,25 @@ def test_evict_rejects(over, status):
     assert _status(_evict, **over) == status
 
 
+@pytest.mark.parametrize("what", [b"\0" * 16, "0123456789abcdef", bytearray(16), 1.0, [1, 2], object()],
+                         ids=["bytes", "str", "bytearray", "float", "list", "object"])
+def test_what_is_no_array_is_refused(what):
+    """Neither the text's bytes nor the object's own memory become an address."""
+    for call, name in ((_norm_rope, "q"), (_norm_rope, "pos"), (_append, "lens"), (_append, "k"), (_read, "k_out"),
+                       (_attn, "workspace"), (_attn, "table"), (_evict, "weights")):
+        with pytest.raises(AttributeError):
+            call(**{name: what})
+    with pytest.raises(AttributeError):  # an entry point of the prompt's path
+        kvb.kvb_deviation(1, 1, 64, 1, what, FAKE, FAKE, FAKE, 0, FAKE, stream=0)
+
+
+@pytest.mark.skipif(not NO_GPU, reason="would launch")
+def test_addresses_and_host_arrays_are_taken():
+    for what in (FAKE, True * FAKE, np.zeros(16, np.float32)):
+        with pytest.raises(kvb.KvbError):
+            _norm_rope(pos=what)
+
+
 def test_attn_workspace_is_pure():
     lay = _layout(max_blocks=4096, n_blocks=100000)
     f = kvb.kvb_cache8_attn_workspace_bytes
