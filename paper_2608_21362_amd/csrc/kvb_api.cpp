@@ -833,10 +833,12 @@ kvb_status kvb_cache8_evict(const kvb_cache8_layout* layout, int32_t n_layers, i
   if (kvb_status s = check_cache8_rows(layout, n_layers, n_seqs)) return s;
   REQUIRE(n_first >= 0 && n_recent >= 0 && (int64_t)n_first + n_recent <= budget,
           "n_first and n_recent must be non-negative and fit the budget");
-  const void* ptrs[] = {table, lens, weights, table_out, lens_out, weights_out};
-  for (const void* p : ptrs) REQUIRE(p != nullptr, "a required pointer is NULL");
-  REQUIRE(table != table_out && lens != lens_out && weights != weights_out,
-          "an output is an input");
+  const void *in[] = {table, lens, weights}, *out[] = {table_out, lens_out, weights_out};
+  for (const void* p : in) REQUIRE(p != nullptr, "a required pointer is NULL");
+  for (const void* p : out) {
+    REQUIRE(p != nullptr, "a required pointer is NULL");
+    for (const void* x : in) REQUIRE(p != x, "an output is an input");
+  }
   kvb::Evict a{};
   a.n_seqs = n_seqs, a.n_kv_heads = layout->n_kv_heads, a.block_len = layout->block_len;
   a.max_blocks = layout->max_blocks, a.budget = budget, a.n_first = n_first, a.n_recent = n_recent;

@@ -198,6 +198,13 @@ def test_evict_rejects(over, status):
     assert _status(_evict, **over) == status
 
 
+@pytest.mark.parametrize("out", ["table_out", "lens_out", "weights_out"])
+@pytest.mark.parametrize("into", ["table", "lens", "weights"])
+def test_evict_rejects_every_input_as_an_output(out, into):
+    apart = dict(table=FAKE, lens=2 * FAKE, weights=3 * FAKE, table_out=4 * FAKE, lens_out=5 * FAKE, weights_out=6 * FAKE)
+    assert _status(_evict, **{**apart, out: apart[into]}) == EINVAL
+
+
 @pytest.mark.parametrize("what", [b"\0" * 16, "0123456789abcdef", bytearray(16), 1.0, [1, 2], object()],
                          ids=["bytes", "str", "bytearray", "float", "list", "object"])
 def test_what_is_no_array_is_refused(what):
