@@ -500,7 +500,8 @@ typedef enum { KVB_PAIR_HALF = 0, KVB_PAIR_INTERLEAVED = 1 } kvb_pairing;
  * for the pairs (a, b) of the first rot_dim channels, with (c, s) row pos[t] of
  * the tables (f32 [table_len][rot_dim/2]); the other channels are y.  Arithmetic
  * is float, rounded once to dtype (KVB_BF16 or KVB_F32, of inputs and outputs
- * alike); squares are summed in float, so values of a normed head are below 1e18.
+ * alike); squares are summed in float, so values of a normed head are below 1e18
+ * (and, where eps is 0, the largest above 1e-17).
  * A token whose position lies outside [0, table_len) is written as NaN.
  * Element (t, h, c) of each tensor lies at t * token_stride + h * head_stride +
  * c, strides in elements, multiples of 8: the input may be one projection's
@@ -566,6 +567,11 @@ typedef struct {
  * they hold.  A sequence without new rows is left alone, one with lens[b] < n_new
  * as well.  max_new bounds the new rows of a sequence (it sizes the grid).
  * cu_new i32 [n_seqs+1].  A table must not name a block twice.
+ * Rows can be taken back by a smaller lens[b] as long as none of them completed a
+ * block: a block is quantised with all of its rows, and the tails then hold the
+ * next one's.  A caller that appends rows which may be rejected (drafted tokens)
+ * keeps a copy of the tails, puts it back, and appends the accepted rows again
+ * from the old length; the block is then written anew.
  * Errors: KVB_EINVAL, KVB_EUNSUPPORTED (layout). */
 kvb_status kvb_cache8_append(const kvb_cache8_layout* layout, int32_t n_layers, int32_t n_seqs,
                              const int32_t* cu_new, int32_t max_new, const uint16_t* k,
@@ -611,9 +617,20 @@ size_t kvb_cache8_attn_workspace_bytes(const kvb_cache8_layout* layout, int32_t 
  * is scaled to fp16 by a power of two, which is exact but for values below 2^-14
  * of its largest), softmax, weights and sums in float; the probabilities enter
  * the product with V as fp16, those of the tails as the sum of two bfloat16.
- * softmax_scale is any finite number.
+ * softmax_scale is any finite number with which its product with the norms of a
+ * query and a key (or 1, if the key's is smaller) stays below 2^125.
+ * That fp16 number is a probability times the scale of its block of V over the
+ * largest of the blocks that were read with it, some of which the query may not
+ * see.  So beside 2^-11 of its term a token adds at most 2^-29 of the largest |V|
+ * of the sequence's full blocks of that kv head (or of 2^-80, if that is larger)
+ * to the error of out: with all the weight on blocks 2^-20 of the largest, out
+ * begins to lose bits, and from 2^-31 on it is 0.  lse and the weights do not
+ * depend on V.
  * max_queries bounds n_q, max_len bounds lens (they size the grid; results
  * do not depend on max_len but for the order of the sums).  Deterministic.
+ * With weights the workspace holds a float for every query row and part of up to
+ * 64 tokens of the whole table (lens may pass max_len): n_seqs * Hq * max_queries
+ * * (max_blocks + 1) * max(1, B / 64) of them.
  * workspace: at least kvb_cache8_attn_workspace_bytes; calls that share it must be ordered.
  * Errors: KVB_EINVAL (incl. workspace too small, Hq % Hkv != 0), KVB_EUNSUPPORTED
  * (layout). */

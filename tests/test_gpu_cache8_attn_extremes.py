@@ -125,3 +125,22 @@ def test_values_near_the_end_of_the_range(coded, tail, nq, claim, code):
     q = torch.from_numpy(_normal(16, nq, 4, d)).bfloat16().cuda()
     out, lse, w, win = _attend(c, q, nq, claim)
     check_attention(c, q, [nq], out, lse, w, win, sharp=coded != tail)
+
+
+@CODES
+@KINDS
+@pytest.mark.parametrize("before", [True, False], ids=["large_first", "small_first"])
+@pytest.mark.parametrize("down", [20, 24, 28, 32])
+def test_weight_on_a_block_of_small_values(down, before, nq, claim, code):
+    """Nearly all of the weight on a block 2^-down of the others: within what a key may add, 2^-29 of the largest value."""
+    _say(f"V down by 2^{down} large first {before} queries {nq} max_len {claim} code {code}")
+    T, d, B, at = 700, 128, 64, 448 if before else 64
+    c = Cache([T], 1, d, B, code, seed=2)
+    k, v = _normal(5, T, d), _normal(6, T, d)
+    v[at:at + B] *= np.float32(2.0 ** -down)
+    u = _normal(7, d)
+    k[at + 7] = od.bf16(u * 2)
+    c.put(0, 0, 0, k, v)
+    q = torch.from_numpy(np.broadcast_to(u, (nq, 4, d)).copy()).bfloat16().cuda()
+    out, lse, w, win = _attend(c, q, nq, claim)
+    check_attention(c, q, [nq], out, lse, w, win, sharp=True)

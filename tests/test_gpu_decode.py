@@ -238,6 +238,52 @@ def test_a_stitched_prompt_is_packed_and_decoded():
             assert abs(lse[0, hq].item() - e[0]) <= 2.0 ** -12 * max(1, abs(e[0]))
 
 
+@pytest.mark.parametrize("code", [od.I8, od.E4M3], ids=["i8", "e4m3"])
+def test_drafted_rows_are_taken_back(code):
+    """Five drafted tokens, two of which are accepted: over a block's border the tails' copy comes back and the
+    accepted rows are appended again; inside a block a smaller length is enough.  The same bits as without a draft."""
+    from paper_2608_21362_amd import kvb
+
+    H, d, B, lens = 2, 64, 32, [62, 94, 65, 60]  # the border is passed by all five, by the accepted two, or by none
+    k, v = (torch.from_numpy(x).bfloat16().cuda() for x in _prompt(4, H, d, lens, 5))
+    g = torch.Generator("cuda").manual_seed(5)
+    drafted = [torch.randn((4, 5, H, d), generator=g, device="cuda").bfloat16() for _ in range(2)]
+
+    def append(dec, n, lens):
+        rows = [x[:, :n].reshape(4 * n, H, d).contiguous() for x in drafted]
+        dec.lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        kvb.kvb_cache8_append(dec.layout, 1, 4, cu([n] * 4), n, *rows, 0, H * d, d, dec.table, dec.lens, *dec.arrays())
+
+    pair = [Decoder(kvb, lens, 4, H, d, B, code, room=40, seed=1) for _ in range(2)]
+    for dec in pair:
+        dec.pack(k, v, lens)
+    held = [t.clone() for t in pair[0].tails]
+    append(pair[0], 5, [n + 5 for n in lens])
+    for t, was in zip(pair[0].tails, held):
+        t.copy_(was)
+    for dec in pair:
+        append(dec, 2, [n + 2 for n in lens])
+    back = []
+    for dec in pair:
+        T = sum(lens) + 8
+        out = [torch.zeros((1, H, T, d), device="cuda") for _ in range(2)]
+        kvb.kvb_cache8_read(dec.layout, 1, 4, cu([n + 2 for n in lens]), max(lens) + 2, dec.table, dec.lens, *dec.arrays(),
+                            kvb.KVB_F32, *out, H * T * d, d, T * d)
+        back.append(out)
+    assert all(torch.equal(a, b) for a, b in zip(*back))
+    # the third and the fourth sequence passed no border with the draft or with its first rows: the length is enough
+    dec = Decoder(kvb, lens, 4, H, d, B, code, room=40, seed=1)
+    dec.pack(k, v, lens)
+    append(dec, 3, [n + 3 for n in lens])
+    dec.lens.copy_(torch.tensor([n + 2 for n in lens], dtype=torch.int32))
+    T = sum(lens) + 8
+    out = [torch.zeros((1, H, T, d), device="cuda") for _ in range(2)]
+    kvb.kvb_cache8_read(dec.layout, 1, 4, cu([n + 2 for n in lens]), max(lens) + 2, dec.table, dec.lens, *dec.arrays(),
+                        kvb.KVB_F32, *out, H * T * d, d, T * d)
+    inside = slice(sum(lens[:2]) + 4, T)
+    assert all(torch.equal(a[:, :, inside], b[:, :, inside]) for a, b in zip(out, back[1]))
+
+
 def test_captured_steps_replayed_in_turn():
     """Two captured decoders with buffers of their own, replayed in turn, each replay after eager work and a
     synchronisation, against an eager decoder fed with the same tokens: equal bits throughout."""
