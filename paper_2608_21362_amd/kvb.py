@@ -359,7 +359,7 @@ def kvb_qk_norm_rope(n_tokens, n_q_heads, n_kv_heads, head_dim, dtype, q, q_toke
                      k_out_head_stride, stream=None):
     _check(_lib.kvb_qk_norm_rope(n_tokens, n_q_heads, n_kv_heads, head_dim, dtype, _p(q),
                                  q_token_stride, q_head_stride, _p(k), k_token_stride,
-                                 k_head_stride, _p(q_weight), _p(k_weight), float(eps), _p(pos),
+                                 k_head_stride, _p(q_weight), _p(k_weight), eps, _p(pos),
                                  _p(table_cos), _p(table_sin), table_len, rot_dim, pairing,
                                  _p(q_out), q_out_token_stride, q_out_head_stride, _p(k_out),
                                  k_out_token_stride, k_out_head_stride, _stream(stream)))
@@ -396,8 +396,8 @@ def kvb_cache8_attn(layout, n_q_heads, n_seqs, cu_q, n_queries, max_queries, max
     _check(_lib.kvb_cache8_attn(ctypes.byref(layout), n_q_heads, n_seqs, _p(cu_q), n_queries,
                                 max_queries, max_len, _p(q), _p(table), _p(lens), _p(k_codes),
                                 _p(k_scale), _p(v_codes), _p(v_scale), _p(k_tail), _p(v_tail),
-                                float(softmax_scale), _p(out), _p(lse), _p(weights_in),
-                                _p(weights_out), _p(workspace), workspace_bytes, _stream(stream)))
+                                softmax_scale, _p(out), _p(lse), _p(weights_in), _p(weights_out),
+                                _p(workspace), workspace_bytes, _stream(stream)))
 
 
 def kvb_cache8_evict(layout, n_layers, n_seqs, budget, n_first, n_recent, table, lens, weights,

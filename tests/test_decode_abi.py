@@ -224,14 +224,6 @@ def test_addresses_and_host_arrays_are_taken():
             _norm_rope(pos=what)
 
 
-@pytest.mark.skipif(not NO_GPU, reason="would launch")
-@pytest.mark.parametrize("number", [np.float32(0.125), np.float64(0.125), torch.tensor(0.125), 1])
-def test_numbers_of_any_kind_are_taken(number):
-    """As by the prompt's attention: every check passes."""
-    assert _status(_attn, softmax_scale=number) == kvb.KVB_EHIP
-    assert _status(_norm_rope, eps=number) == kvb.KVB_EHIP
-
-
 def test_attn_workspace_is_pure():
     lay = _layout(max_blocks=4096, n_blocks=100000)
     f = kvb.kvb_cache8_attn_workspace_bytes
