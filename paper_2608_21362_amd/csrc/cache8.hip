@@ -549,14 +549,13 @@ __global__ void __launch_bounds__(256) evict_wave_kernel(Evict a, int64_t rows) 
 // kept and dropped entries from ballots.  Counts decide, so the result does not depend on the
 // order of the atomics.
 constexpr int kEvictWaves = 16;
-constexpr int64_t kEvictX = 1 << 21;  // grid rows in x, the others in y: a dimension holds less than 2^32 work items
-__global__ void __launch_bounds__(64 * kEvictWaves) evict_kernel(Evict a, int64_t rows) {
+constexpr int64_t kEvictRows = 1 << 21;  // of a launch: a grid dimension holds less than 2^32 work items
+__global__ void __launch_bounds__(64 * kEvictWaves) evict_kernel(Evict a, int first) {
   constexpr int T = 64 * kEvictWaves;
   __shared__ int32_t bins[256], wave_kept[kEvictWaves], wave_ties[kEvictWaves];
   __shared__ uint32_t s_prefix;
   __shared__ int32_t s_left;
-  const int64_t row = blockIdx.y * kEvictX + blockIdx.x;
-  if (row >= rows) return;
+  const int64_t row = first + blockIdx.x;
   const int b = (int)((uint32_t)row / (uint32_t)a.n_kv_heads % (uint32_t)a.n_seqs);
   const int M = a.max_blocks, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int32_t* table = a.table + row * M;
@@ -718,10 +717,12 @@ hipError_t launch_cache8_evict(const Evict& a, int n_layers, hipStream_t s) {
   // A workgroup a row where a wave cannot hold it, and where a long row would be one wave's on an
   // empty card (72 rows of 512 / 1024 entries: 9.7 / 17.5 us by waves, 6.8 / 7.2 so; of 256 6.1 and
   // 6.6; 300 rows 10.1 / 18.9 and 11.7 / 12.6; 1200 rows 11.5 / 21.5 and 28.5 / 30.9).
-  if (a.max_blocks > 2048 || (a.max_blocks > 256 && rows <= 256))
-    hipLaunchKernelGGL(evict_kernel, dim3((unsigned)(rows < kEvictX ? rows : kEvictX), (unsigned)((rows + kEvictX - 1) / kEvictX)),
-                       dim3(64 * kEvictWaves), 0, s, a, rows);
-  else if (a.max_blocks <= 256) KVB_EVICT(4);
+  if (a.max_blocks > 2048 || (a.max_blocks > 256 && rows <= 256)) {
+    for (int64_t first = 0; first < rows; first += kEvictRows) {
+      const int64_t n = rows - first < kEvictRows ? rows - first : kEvictRows;
+      hipLaunchKernelGGL(evict_kernel, dim3((unsigned)n), dim3(64 * kEvictWaves), 0, s, a, (int)first);
+    }
+  } else if (a.max_blocks <= 256) KVB_EVICT(4);
   else if (a.max_blocks <= 512) KVB_EVICT(8);
   else if (a.max_blocks <= 1024) KVB_EVICT(16);
   else KVB_EVICT(32);
