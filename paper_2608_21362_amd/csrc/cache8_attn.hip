@@ -6,7 +6,9 @@ namespace kvb {
 namespace {
 
 constexpr int kCus = 256;
-constexpr unsigned kFinishX = 1 << 22;
+// workgroups of a launch that joins and adds weights: a long table takes several (work items of a grid
+// dimension past 2^32 are lost)
+constexpr int kFinishX = 1 << 22;
 // tiles stay small up to this many rows, and may up to this many rows x keys of a call
 constexpr int kFewRows = 128;
 constexpr int64_t kFewWork = 1 << 25;
@@ -185,9 +187,8 @@ template <int D, int B, bool MANY>
 __global__ void __launch_bounds__(256) attn8_finish_kernel(Attn8 a, Attn8Plan plan,
                                                            const float* __restrict__ po,
                                                            const float* __restrict__ ml,
-                                                           const float* __restrict__ parts) {
-  const int wg = (int)(blockIdx.z * gridDim.x + blockIdx.x);
-  if (wg >= plan.join_wgs + plan.weight_wgs) return;
+                                                           const float* __restrict__ parts, int first) {
+  const int wg = first + blockIdx.x;
   if (wg < plan.join_wgs) join<D, B, MANY>(a, plan, blockIdx.y, wg, po, ml);
   else if (plan.weight_lanes == 256) add_weights_of_many<B>(a, plan, blockIdx.y, wg - plan.join_wgs, ml, parts);
   else add_weights<B>(a, plan, blockIdx.y, wg - plan.join_wgs, ml, parts);
@@ -199,21 +200,21 @@ __global__ void __launch_bounds__(256) attn8_finish_kernel(Attn8 a, Attn8Plan pl
 bool few_splits(const Attn8Plan& plan) { return plan.n_splits <= (plan.rows > 1024 ? 8 : 4); }
 
 template <int D, int B>
-void finish(const Attn8Plan& plan, const Attn8& a, dim3 grid, const float* po, const float* ml,
+void finish(const Attn8Plan& plan, const Attn8& a, dim3 grid, int first, const float* po, const float* ml,
             const float* parts, hipStream_t s) {
   if (!few_splits(plan))
-    hipLaunchKernelGGL((attn8_finish_kernel<D, B, true>), grid, dim3(256), 0, s, a, plan, po, ml, parts);
+    hipLaunchKernelGGL((attn8_finish_kernel<D, B, true>), grid, dim3(256), 0, s, a, plan, po, ml, parts, first);
   else
-    hipLaunchKernelGGL((attn8_finish_kernel<D, B, false>), grid, dim3(256), 0, s, a, plan, po, ml, parts);
+    hipLaunchKernelGGL((attn8_finish_kernel<D, B, false>), grid, dim3(256), 0, s, a, plan, po, ml, parts, first);
 }
 
 template <int D>
-void finish(const Attn8Plan& plan, const Attn8& a, int block_len, dim3 grid, const float* po,
+void finish(const Attn8Plan& plan, const Attn8& a, int block_len, dim3 grid, int first, const float* po,
             const float* ml, const float* parts, hipStream_t s) {
-  if (block_len == 16) finish<D, 16>(plan, a, grid, po, ml, parts, s);
-  else if (block_len == 32) finish<D, 32>(plan, a, grid, po, ml, parts, s);
-  else if (block_len == 64) finish<D, 64>(plan, a, grid, po, ml, parts, s);
-  else finish<D, 128>(plan, a, grid, po, ml, parts, s);
+  if (block_len == 16) finish<D, 16>(plan, a, grid, first, po, ml, parts, s);
+  else if (block_len == 32) finish<D, 32>(plan, a, grid, first, po, ml, parts, s);
+  else if (block_len == 64) finish<D, 64>(plan, a, grid, first, po, ml, parts, s);
+  else finish<D, 128>(plan, a, grid, first, po, ml, parts, s);
 }
 
 }  // namespace
@@ -293,12 +294,12 @@ hipError_t launch_cache8_attn(const Attn8Plan& plan, const Attn8& a, int head_di
   kernels(plan, a, block_len, po, ml, parts, s);
   if (hipError_t e = hipGetLastError()) return e;
   if (plan.join_wgs + plan.weight_wgs == 0) return hipSuccess;
-  // up to 2^22 workgroups in x, the others in z: a long table has more than 2^32 / 256 (work items of a
-  // grid dimension past 2^32 are lost)
-  const unsigned wgs = (unsigned)(plan.join_wgs + plan.weight_wgs), across = wgs < kFinishX ? wgs : kFinishX;
-  const dim3 grid(across, (unsigned)(a.c.n_seqs * a.c.n_kv_heads), (wgs + across - 1) / across);
-  if (head_dim == 128) finish<128>(plan, a, block_len, grid, po, ml, parts, s);
-  else finish<64>(plan, a, block_len, grid, po, ml, parts, s);
+  const int wgs = plan.join_wgs + plan.weight_wgs;
+  for (int first = 0; first < wgs; first += kFinishX) {
+    const dim3 grid((unsigned)(wgs - first < kFinishX ? wgs - first : kFinishX), (unsigned)(a.c.n_seqs * a.c.n_kv_heads));
+    if (head_dim == 128) finish<128>(plan, a, block_len, grid, first, po, ml, parts, s);
+    else finish<64>(plan, a, block_len, grid, first, po, ml, parts, s);
+  }
   return hipGetLastError();
 }
 
