@@ -651,7 +651,7 @@ struct Chunk {
 // (i + 1) widened into LDS, loads of the next ones; waves 4 to 7 are one run behind waves 0 to 3,
 // and a barrier ends every run.  Three slots: a slot is written two runs before it is read and two
 // runs after it was.  2048 queries of 16 heads, 32K tokens of 2 (533 GFLOP): 522 us, 1020
-// TFLOP/s; with 4 waves a workgroup, 2 workgroups a CU and every wave free to run, both kinds of
+// TFLOP/s in a row of such calls (600 to 620 in the first ones after a rest); with 4 waves a workgroup, 2 workgroups a CU and every wave free to run, both kinds of
 // work took turns by chance: 601 us.  Either kind alone takes 330 to 350 us.
 template <int D, int B, int CODE, bool WEIGHTS>
 __global__ void __launch_bounds__(512, 2)
