@@ -622,7 +622,7 @@ size_t kvb_cache8_attn_workspace_bytes(const kvb_cache8_layout* layout, int32_t 
  * That fp16 number is a probability times the scale of its block of V over the
  * largest of the blocks that were read with it, some of which the query may not
  * see.  So beside 2^-11 of its term a token adds at most 2^-29 of the largest |V|
- * of the sequence's full blocks of that kv head (or of 2^-80, if that is larger)
+ * of the sequence's full blocks of that kv head (or of 2^-90, if that is larger)
  * to the error of out: with all the weight on blocks 2^-20 of the largest, out
  * begins to lose bits, and from 2^-31 on it is 0.  lse and the weights do not
  * depend on V.

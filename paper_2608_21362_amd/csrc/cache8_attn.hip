@@ -22,8 +22,8 @@ __device__ __forceinline__ int splits_of(const Seq& sq, const Attn8Plan& plan, i
   return max(1, min(k, plan.n_splits));
 }
 
-// Joins the splits of the rows.  MANY: a workgroup a row; the sums of the splits are weighed first (a
-// lane a split), then D / 4 lanes a split add their outputs, 256 / (D / 4) splits at a time.
+// Joins the splits of the rows, each divided by its own sum.  MANY: a workgroup a row; the sums of the splits
+// are weighed first (a lane a split), then D / 4 lanes a split add their outputs, 256 / (D / 4) splits at a time.
 // Otherwise D / 4 lanes a row take its few splits one after another.  Either way the sizes fix the
 // order of the sums.
 template <int D, int B, bool MANY>
@@ -52,27 +52,32 @@ __device__ __forceinline__ void join(const Attn8& a, const Attn8Plan& plan, int 
     if ((tid & 63) == 0) wave_top[tid >> 6] = top;
     __syncthreads();
     top = fmaxf(fmaxf(wave_top[0], wave_top[1]), fmaxf(wave_top[2], wave_top[3]));
-    const float f = tid < n ? __builtin_amdgcn_exp2f(m - top) : 0.f;
-    weight[tid] = f;
-    sum = f * l;
+    sum = tid < n ? __builtin_amdgcn_exp2f(m - top) * l : 0.f;
+    weight[tid] = sum;
     for (int k = 1; k < 64; k <<= 1) sum += __shfl_xor(sum, k, 64);
     if ((tid & 63) == 0) wave_sum[tid >> 6] = sum;
     __syncthreads();
     sum = wave_sum[0] + wave_sum[1] + wave_sum[2] + wave_sum[3];
+    const float inv = inverse(sum);
 #pragma unroll 4
     for (int s = sg; s < n; s += SG)
-      x += weight[s] * *reinterpret_cast<const f4_t*>(po + (rec + (int64_t)s * plan.rows) * D + c * 4);
+      x += weight[s] * inv * *reinterpret_cast<const f4_t*>(po + (rec + (int64_t)s * plan.rows) * D + c * 4);
     sums[sg][c] = x;
     __syncthreads();
     if (tid >= LPR) return;
     for (int s = 1; s < SG; ++s) x += sums[s][c];
   } else {
     if (!in) return;
-    for (int s = 0; s < n; ++s) top = fmaxf(top, ml[2 * (rec + (int64_t)s * plan.rows)]);
+    for (int s = 0; s < n; ++s) {
+      const float2 y = *reinterpret_cast<const float2*>(ml + 2 * (rec + (int64_t)s * plan.rows));
+      const float next = fmaxf(top, y.x);
+      sum = sum * __builtin_amdgcn_exp2f(top - next) + y.y * __builtin_amdgcn_exp2f(y.x - next);
+      top = next;
+    }
+    const float inv = inverse(sum);
     for (int s = 0; s < n; ++s) {
       const int64_t at = rec + (int64_t)s * plan.rows;
-      const float f = __builtin_amdgcn_exp2f(ml[2 * at] - top);
-      sum += f * ml[2 * at + 1];
+      const float f = __builtin_amdgcn_exp2f(ml[2 * at] - top) * ml[2 * at + 1] * inv;
       x += f * *reinterpret_cast<const f4_t*>(po + at * D + c * 4);
     }
   }

@@ -47,9 +47,6 @@ constexpr float kSlack = 8.f;     // the running maximum follows once it is off 
 constexpr float kFar = 0x1p20f;   // below it a score's rounding (2^-4 at most) is no matter to 2^score's range
 constexpr int kScaleTop = 6;      // weights of V scales stay below 2^kScaleTop
 constexpr int kTailTop = 16;      // outputs' unit (log2) over a tail, at least
-// Outputs leave a wave 2^-kGuard of their size: a sum of probabilities is below 2^39 (2^30 keys, 2^kSlack
-// each), so no sum of them times V leaves a float that V itself fits.
-constexpr int kGuard = 40;
 constexpr int kManyTile = 256;  // rows of a tile of the many-rows kernel
 
 // four codes -> four fp16 numbers
@@ -146,13 +143,16 @@ __device__ __forceinline__ Place place(const Attn8& a, const Attn8Plan& plan) {
   return {z < a.c.n_rows ? z : -1, group - z * plan.n_splits, (int)blockIdx.x / kXcds};
 }
 
-// One row's result: 2^kGuard x / sum in bfloat16, and the log of the sum.
+// Outputs are divided by their sums before they leave a wave, and joined by weights whose sum is 1, so that
+// nothing passes the largest value of V (a sum of probabilities, up to 2^8 a key, times V may leave a float).
+// A reciprocal within 2^-23 will do (a token over 2000: 11.67 us, with quotients 11.75).
+__device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum); }
+
+// One row's result x in bfloat16, and the log of its sum.
 __device__ __forceinline__ void write_row(const Attn8& a, int q, int head, int D, int c, f4_t x,
                                           float top, float sum) {
-  const float inv = sum == 0.f ? 0.f : __builtin_ldexpf(1.f / sum, kGuard);
   const int64_t r = (int64_t)q * a.n_q_heads + head;
-  *reinterpret_cast<uint2*>(a.out + r * D + c) =
-      make_uint2(pack_bf16x2(x[0] * inv, x[1] * inv), pack_bf16x2(x[2] * inv, x[3] * inv));
+  *reinterpret_cast<uint2*>(a.out + r * D + c) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
   if (a.lse && c == 0) a.lse[r] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
 
@@ -581,14 +581,15 @@ attn8_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __restrict_
     r.tail(a, sq, z, h, G, row0, r0, lane);
 
   // the waves meet
-  const float unit = __builtin_ldexpf(1.f, r.vexp - kScaleTop - kGuard);
+  const float unit = __builtin_ldexpf(1.f, r.vexp - kScaleTop);
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     r.l[n] = sum4groups(r.l[n]);
+    const float inv = inverse(r.l[n]);
     if (grp == 0) part_ml[wave][n * 16 + col][0] = r.m[n], part_ml[wave][n * 16 + col][1] = r.l[n];
 #pragma unroll
     for (int c = 0; c < CT; ++c)
-      *reinterpret_cast<f4_t*>(&part_o[wave][n * 16 + col][c * 16 + grp * 4]) = r.o[n][c] * unit;
+      *reinterpret_cast<f4_t*>(&part_o[wave][n * 16 + col][c * 16 + grp * 4]) = r.o[n][c] * inv * unit;
   }
   __syncthreads();
   constexpr int LPR = D / 4;  // lanes of a row
@@ -601,14 +602,16 @@ attn8_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __restrict_
     float top = part_ml[0][rr][0];
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) top = fmaxf(top, part_ml[w][rr][0]);
-    float sum = 0.f;
-    f4_t x = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f, f[WAVES];
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
-      const float f = __builtin_amdgcn_exp2f(part_ml[w][rr][0] - top);
-      sum += f * part_ml[w][rr][1];
-      x += f * *reinterpret_cast<const f4_t*>(&part_o[w][rr][c]);
+      f[w] = __builtin_amdgcn_exp2f(part_ml[w][rr][0] - top) * part_ml[w][rr][1];
+      sum += f[w];
     }
+    const float inv = inverse(sum);
+    f4_t x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) x += f[w] * inv * *reinterpret_cast<const f4_t*>(&part_o[w][rr][c]);
     const int64_t rec = ((int64_t)z * plan.n_splits + split) * plan.rows + row;
     if ((!whole || WEIGHTS) && c == 0) ml[2 * rec] = top, ml[2 * rec + 1] = sum;
     if (!whole) {
@@ -847,12 +850,12 @@ attn8_tile_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __rest
   if (split == 0)
     for (int r0 = 0; r0 < B && sq.full * B + r0 < seen_by(sq, last); r0 += 64) r.tail(a, sq, z, h, G, wrow0, r0, lane);
 
-  const float unit = __builtin_ldexpf(1.f, r.vexp - kScaleTop - kGuard);
+  const float unit = __builtin_ldexpf(1.f, r.vexp - kScaleTop);
   const bool whole = plan.n_splits == 1;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     const int row = wrow0 + n * 16 + col;
-    const float sum = sum4groups(r.l[n]);
+    const float sum = sum4groups(r.l[n]), inv = inverse(sum);
     if (row >= sq.n_q * G || row >= plan.rows) continue;
     const int64_t rec = ((int64_t)z * plan.n_splits + split) * plan.rows + row;
     if ((!whole || WEIGHTS) && grp == 0) ml[2 * rec] = r.m[n], ml[2 * rec + 1] = sum;
@@ -860,8 +863,9 @@ attn8_tile_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __rest
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
       const int ch = c * 16 + grp * 4;
-      if (whole) write_row(a, sq.q0 + i, h * G + row - i * G, D, ch, r.o[n][c] * unit, r.m[n], sum);
-      else *reinterpret_cast<f4_t*>(po + rec * D + ch) = r.o[n][c] * unit;
+      const f4_t x = r.o[n][c] * inv * unit;
+      if (whole) write_row(a, sq.q0 + i, h * G + row - i * G, D, ch, x, r.m[n], sum);
+      else *reinterpret_cast<f4_t*>(po + rec * D + ch) = x;
     }
   }
 }

@@ -144,3 +144,28 @@ def test_weight_on_a_block_of_small_values(down, before, nq, claim, code):
     q = torch.from_numpy(np.broadcast_to(u, (nq, 4, d)).copy()).bfloat16().cuda()
     out, lse, w, win = _attend(c, q, nq, claim)
     check_attention(c, q, [nq], out, lse, w, win, sharp=True)
+
+
+@CODES
+@KINDS
+@pytest.mark.parametrize("coded,tail", [(1.0, 1.0), (0.0, 1.0), (1.0, 0.0)], ids=["both", "tail", "coded"])
+def test_small_values_keep_their_bits(coded, tail, nq, claim, code):
+    """V of the size 2^-100.  Beside the bounds of check_attention a key of a full block adds what fp16 drops:
+    2^-25 in units of 2^-106, times a code of up to 448."""
+    _say(f"V 2^-100 coded {coded} tail {tail} queries {nq} max_len {claim} code {code}")
+    T, d, B = 700, 128, 64
+    c = Cache([T], 1, d, B, code, seed=6)
+    k, v = _normal(17, T, d), _normal(18, T, d).astype(np.float64) * 2.0 ** -100
+    v[:T // B * B] *= coded
+    v[T // B * B:] *= tail
+    c.put(0, 0, 0, k, od.bf16(v))
+    q = torch.from_numpy(_normal(19, nq, 4, d)).bfloat16().cuda()
+    out, lse, w, win = _attend(c, q, nq, claim)
+    got, q = out.double().cpu().numpy(), q.double().cpu().numpy()
+    for h in range(4):
+        o, _, p = od.attention(q[:, h], c.k[0, 0, 0], c.v[0, 0, 0], d ** -0.5)
+        off = 2.0 ** -24 * (d + 8) * d ** -0.5 * (np.abs(q[:, h]) @ np.abs(c.k[0, 0, 0]).T).max(1)
+        off = off + 2.0 ** -25 * d ** -0.5 * np.abs(q[:, h]).max(1) * np.abs(c.k[0, 0, 0]).sum(1).max()
+        near = p @ np.abs(c.v[0, 0, 0]) * (2.0 ** -11 + 2 * off + 2.0 ** -20)[:, None] + 2.0 ** -8 * np.abs(o)
+        near = near + coded * T * 448 * 2.0 ** -131
+        assert np.all(np.abs(got[:, h] - o) <= near), (h, float((np.abs(got[:, h] - o) / near).max()))
