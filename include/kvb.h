@@ -567,11 +567,11 @@ typedef struct {
  * they hold.  A sequence without new rows is left alone, one with lens[b] < n_new
  * as well.  max_new bounds the new rows of a sequence (it sizes the grid).
  * cu_new i32 [n_seqs+1].  A table must not name a block twice.
- * Rows can be taken back by a smaller lens[b] as long as none of them completed a
- * block: a block is quantised with all of its rows, and the tails then hold the
- * next one's.  A caller that appends rows which may be rejected (drafted tokens)
- * keeps a copy of the tails, puts it back, and appends the accepted rows again
- * from the old length; the block is then written anew.
+ * Rows can be taken back by a smaller lens[b] as long as floor(lens[b] / B) stays
+ * the same: a full block is quantised with all of its rows, and the tails then
+ * hold the next one's.  A caller that appends rows which may be rejected (drafted
+ * tokens) keeps a copy of the tails, puts it back, and appends the accepted rows
+ * again from the old length; the block is then written anew.
  * Errors: KVB_EINVAL, KVB_EUNSUPPORTED (layout). */
 kvb_status kvb_cache8_append(const kvb_cache8_layout* layout, int32_t n_layers, int32_t n_seqs,
                              const int32_t* cu_new, int32_t max_new, const uint16_t* k,
@@ -624,8 +624,8 @@ size_t kvb_cache8_attn_workspace_bytes(const kvb_cache8_layout* layout, int32_t 
  * see.  So beside 2^-11 of its term a token adds at most 2^-29 of the largest |V|
  * of the sequence's full blocks of that kv head (or of 2^-90, if that is larger)
  * to the error of out: with all the weight on blocks 2^-20 of the largest, out
- * begins to lose bits, and from 2^-31 on it is 0.  lse and the weights do not
- * depend on V.
+ * begins to lose bits, and from 2^-31 on it is 0.  lse and the weights depend on
+ * V by the last roundings of a float alone.
  * max_queries bounds n_q, max_len bounds lens (they size the grid; results
  * do not depend on max_len but for the order of the sums).  Deterministic.
  * With weights the workspace holds a float for every query row and part of up to

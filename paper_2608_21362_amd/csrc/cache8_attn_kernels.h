@@ -47,7 +47,7 @@ constexpr float kSlack = 8.f;     // the running maximum follows once it is off 
 constexpr float kFar = 0x1p20f;   // below it a score's rounding (2^-4 at most) is no matter to 2^score's range
 constexpr int kScaleTop = 6;      // weights of V scales stay below 2^kScaleTop
 constexpr int kTailTop = 16;      // outputs' unit (log2) over a tail, at least
-constexpr int kManyTile = 256;  // rows of a tile of the many-rows kernel
+constexpr int kManyTile = 256;    // rows of a tile of the many-rows kernel
 
 // four codes -> four fp16 numbers
 template <int CODE>
@@ -654,8 +654,9 @@ struct Chunk {
 // (i + 1) widened into LDS, loads of the next ones; waves 4 to 7 are one run behind waves 0 to 3,
 // and a barrier ends every run.  Three slots: a slot is written two runs before it is read and two
 // runs after it was.  2048 queries of 16 heads, 32K tokens of 2 (533 GFLOP): 522 us, 1020
-// TFLOP/s in a row of such calls (600 to 620 in the first ones after a rest); with 4 waves a workgroup, 2 workgroups a CU and every wave free to run, both kinds of
-// work took turns by chance: 601 us.  Either kind alone takes 330 to 350 us.
+// TFLOP/s in a row of such calls (600 to 620 in the first ones after a rest); with 4 waves a
+// workgroup, 2 workgroups a CU and every wave free to run, both kinds of work took turns by
+// chance: 601 us.  Either kind alone takes 330 to 350 us.
 template <int D, int B, int CODE, bool WEIGHTS>
 __global__ void __launch_bounds__(512, 2)
 attn8_tile_kernel(Attn8 a, Attn8Plan plan, float* __restrict__ po, float* __restrict__ ml,
