@@ -145,7 +145,7 @@ __device__ __forceinline__ Place place(const Attn8& a, const Attn8Plan& plan) {
 
 // Outputs are divided by their sums before they leave a wave, and joined by weights whose sum is 1, so that
 // nothing passes the largest value of V (a sum of probabilities, up to 2^8 a key, times V may leave a float).
-// A reciprocal within 2^-23 will do (a token over 2000: 11.67 us, with quotients 11.75).
+// A reciprocal within 2^-23 will do (0.08 us less than IEEE quotients of a token's 11.5 over 2000).
 __device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum); }
 
 // One row's result x in bfloat16, and the log of its sum.
@@ -653,8 +653,8 @@ struct Chunk {
 // i, and a run of vector work, S(i) = the probabilities of step i, codes of K (step i + 2) and of V
 // (i + 1) widened into LDS, loads of the next ones; waves 4 to 7 are one run behind waves 0 to 3,
 // and a barrier ends every run.  Three slots: a slot is written two runs before it is read and two
-// runs after it was.  2048 queries of 16 heads, 32K tokens of 2 (533 GFLOP): 522 us, 1020
-// TFLOP/s in a row of such calls (600 to 620 in the first ones after a rest); with 4 waves a
+// runs after it was.  2048 queries of 16 heads, 32K tokens of 2 (533 GFLOP): 522 to 526 us,
+// 1020 TFLOP/s, in a row of such calls (600 to 620 in the first ones after a rest); with 4 waves a
 // workgroup, 2 workgroups a CU and every wave free to run, both kinds of work took turns by
 // chance: 601 us.  Either kind alone takes 330 to 350 us.
 template <int D, int B, int CODE, bool WEIGHTS>
